@@ -66,7 +66,11 @@ enum {
                                         max_len_hint the launch was sized for: clamped      */
     ORTHRUS_DEV_APPEND_OVERFLOW = 2, /* cache_len[b]+n_commit[b] > capacity, or n_commit[b]
                                         outside [0,K]: that sequence was not appended       */
-    ORTHRUS_DEV_WAIT_TIMEOUT = 4     /* a bounded hardware wait expired; outputs undefined  */
+    ORTHRUS_DEV_WAIT_TIMEOUT = 4,    /* a bounded hardware wait expired; outputs undefined  */
+    ORTHRUS_DEV_NO_PAGES = 8,        /* orthrus_page_tables: no pages were left for a request, or the
+                                        list of free pages was not one                       */
+    ORTHRUS_DEV_BAD_PAGE = 16        /* a block table or slot map names a page outside the pool: the
+                                        row was not written, or the request's outputs are undefined */
 };
 
 typedef enum { ORTHRUS_BF16 = 0, ORTHRUS_FP32 = 1 } orthrus_dtype_t;
@@ -364,6 +368,142 @@ orthrus_status_t orthrus_rope_block_kv_write(const orthrus_layer_t *layer, const
 orthrus_status_t orthrus_kv_append_layers(const orthrus_layer_t *layers, int32_t n_layers,
         const void *const *k_ar_blks, const void *const *v_ar_blks, const int32_t *n_commit,
         int32_t update_len, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A serving step on a paged cache.
+ *
+ * Requests of unequal and growing length share one pool of pages per layer instead of holding a
+ * capacity each.  One step is
+ *   orthrus_page_tables            pages for the rows that every request adds, and their slots
+ *   orthrus_rope_paged_kv_write    (or orthrus_paged_kv_write) the new rows go to their slots
+ *   orthrus_paged_ar_attend, orthrus_paged_diffusion_attend   attention over a request's pages
+ *   orthrus_sample_tokens          (or a consensus call) the tokens
+ *   orthrus_paged_commit_len       the lengths grow
+ * with the last-but-two per layer; the tables and slots serve all layers.
+ *
+ * Position t of request b lives in page block_table[b][t / page_size], row t % page_size.  A slot is
+ * page * page_size + row, or -1 for a row that does not exist.  Rows of a page at or behind a
+ * request's length are never read.
+ */
+typedef struct {
+    int32_t batch;          /* B >= 1 requests                                      */
+    int32_t n_q_heads;      /* Hq, a multiple of n_kv_heads                         */
+    int32_t n_kv_heads;     /* Hkv                                                  */
+    int32_t head_dim;       /* d in {32, 64, 128, 256}; tensor-core path: 64, 128   */
+    int32_t block;          /* K: rows per request of q and of the new K/V; 1..64 for
+                               the attention calls, 1..2^20 for the writes          */
+    int32_t dtype;          /* orthrus_dtype_t of q, out, new K/V and pages         */
+    int32_t page_size;      /* positions per page, a power of two up to 1024;
+                               tensor-core path: from 16 on                         */
+    int32_t max_pages;      /* width of block_table; max_pages * page_size < 2^31   */
+    int64_t n_pages;        /* pages in the pool, < 2^31                            */
+    void *k_pages;          /* device [n_pages][Hkv][page_size][d]                  */
+    void *v_pages;          /* device [n_pages][Hkv][page_size][d]                  */
+    const int32_t *block_table; /* device [B][max_pages]                            */
+    int32_t *cache_len;     /* device [B]: rows P_b of request b before the block   */
+    const int32_t *n_new;   /* device [B]: rows of the block that exist, 0..K; NULL: all K */
+    int32_t max_len_hint;   /* host upper bound on every P_b; sizes the grid.  0 means
+                               max_pages * page_size - block (or 0).  Longer requests are
+                               served all the same, with fewer CTAs than they would get */
+    float softmax_scale;    /* 0 selects 1/sqrt(head_dim)                           */
+    uint32_t flags;         /* ORTHRUS_LAYER_CACHE_QUIESCENT (the promise covers block_table,
+                               n_new and the pages' rows below cache_len too) and
+                               ORTHRUS_LAYER_NO_EARLY_LAUNCH, as for orthrus_layer_t  */
+} orthrus_paged_layer_t;
+
+/*
+ * Block tables and slot maps from the requests' lengths.  With
+ *   need[b] = ceil((cache_len[b] + n_new[b]) / page_size),
+ * request b, which holds held_in[b] pages, gives back its pages need[b], .., held_in[b] - 1 or takes
+ * need[b] - held_in[b] more, so that it ends with held_out[b] = need[b].  A request that has ended asks
+ * for cache_len = n_new = 0.  free_list[0 .. n_free_in) are the free pages.  Pages that are given back are
+ * put behind them, in the order of requests and pages; then pages are taken from the end of the list, in
+ * the order of requests: request b gets the last ones first.  A request is served if the list is long enough for what it
+ * and all requests before it ask for, served or not; else it keeps held_in[b] pages, granted[b] = 0, and
+ * ORTHRUS_DEV_NO_PAGES is raised.  For a served request granted[b] = n_new[b].
+ *   block_table[b][j], held_in[b] <= j < held_out[b], are written; other entries stay as they are.
+ *   slot_map[b][i] = slot of position cache_len[b] + i for i < granted[b], else -1.
+ * A request with cache_len or n_new below 0, n_new above max_new, held_in outside [0, max_pages] or need
+ * above max_pages is left alone (granted = 0, ORTHRUS_DEV_BAD_CACHE_LEN).  held_out may be held_in, n_free_out may be
+ * n_free_in (in place); nothing else may overlap.  The results do not depend on any order of execution.
+ *   cache_len, n_new, held_in, held_out, granted  device int32 [batch];  block_table  device int32 [batch][max_pages]
+ *   free_list  device int32 [n_pages];  n_free_in, n_free_out  device int32 [1];  slot_map  device int64 [batch][max_new]
+ * 1 <= batch <= 8192, page_size a power of two up to 1024, 1 <= max_new <= 2^24.  `workspace` (status word) may be
+ * NULL.  One launch.
+ */
+orthrus_status_t orthrus_page_tables(int32_t batch, int32_t page_size, int32_t n_pages, int32_t max_pages, int32_t max_new,
+        const int32_t *cache_len, const int32_t *n_new, const int32_t *held_in, int32_t *held_out, int32_t *block_table,
+        int32_t *free_list, const int32_t *n_free_in, int32_t *n_free_out, int32_t *granted, int64_t *slot_map,
+        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The rows of a block go to their slots: for every request b, KV head h and i < K with slot_map[b][i] >= 0,
+ *   k_pages[slot / page_size][h][slot % page_size] = k_blk[b][i][h]   (likewise v), a byte copy.
+ * A slot at or above n_pages * page_size is skipped (ORTHRUS_DEV_BAD_PAGE).  Two rows must not share a slot.
+ * block_table and n_new are not read; cache_len by the rotary form alone.
+ *
+ * orthrus_rope_paged_kv_write: the same with the rotary embedding of orthrus_rope_block_kv_write (same
+ * pairing and angles, position cache_len[b] + i): q_out[b][i] = rotate(q[b][i]) (q_out may be q), keys rotated
+ * on their way, values copied.  Rows without a slot are padding: nothing of them is written, q_out neither.
+ *   slot_map  device int64 [B][K];  k_blk, v_blk  [B][K][Hkv][d];  q, q_out  [B][K][Hq][d]
+ * `workspace` may be NULL.  One launch each.
+ *
+ * orthrus_paged_commit_len: cache_len[b] += n_commit[b]; an n_commit[b] outside [0, K] or a length that would pass
+ * max_pages * page_size leaves that length alone (ORTHRUS_DEV_APPEND_OVERFLOW).
+ */
+orthrus_status_t orthrus_paged_kv_write(const orthrus_paged_layer_t *layer, const int64_t *slot_map, const void *k_blk,
+        const void *v_blk, void *workspace, size_t workspace_bytes, void *stream);
+orthrus_status_t orthrus_rope_paged_kv_write(const orthrus_paged_layer_t *layer, const int64_t *slot_map, const void *q,
+        const void *k_blk, const void *v_blk, float rope_theta, void *q_out, void *workspace, size_t workspace_bytes,
+        void *stream);
+orthrus_status_t orthrus_paged_commit_len(const orthrus_paged_layer_t *layer, const int32_t *n_commit, void *workspace,
+        size_t workspace_bytes, void *stream);
+
+/*
+ * Attention over the pages of a request, whose last rows are the block itself (written before by the calls above): with
+ * n = n_new[b] (K where n_new is NULL), row i < n of request b and query head hq sees
+ *   positions 0 .. P_b + i          (orthrus_paged_ar_attend: plain causal decoding with K = 1, verification of a block),
+ *   positions 0 .. P_b + n - 1      (orthrus_paged_diffusion_attend: the block is bidirectional)
+ * of KV head hq / (Hq / Hkv):  out[b][i][hq] = softmax_j(q[b][i][hq] . key_j * scale) applied to value_j.
+ * Rows i >= n are padding: they are not read and out keeps what it holds there.  q, out: [B][K][Hq][d].
+ *
+ * The work is cut evenly over the GPU whatever the lengths are: CTAs take equal ranges of the batch's tiles of keys, and
+ * the last CTA of a request to finish joins its pieces, in their order, so that results are the same in every run.
+ * A cache_len or n_new out of range is clamped (ORTHRUS_DEV_BAD_CACHE_LEN); a table entry outside the pool among those that
+ * a request needs raises ORTHRUS_DEV_BAD_PAGE, is not followed, and leaves the request's outputs undefined.
+ * Workspace: orthrus_paged_attend_workspace_bytes(layer), initialised by orthrus_workspace_init once.  It depends on the
+ * shape and on max_len_hint, not on the lengths.  1 <= batch <= 16384.
+ */
+size_t orthrus_paged_attend_workspace_bytes(const orthrus_paged_layer_t *layer);
+orthrus_status_t orthrus_paged_ar_attend(const orthrus_paged_layer_t *layer, const void *q, void *out, void *workspace,
+        size_t workspace_bytes, void *stream);
+orthrus_status_t orthrus_paged_diffusion_attend(const orthrus_paged_layer_t *layer, const void *q, void *out, void *workspace,
+        size_t workspace_bytes, void *stream);
+
+/*
+ * One token per row of logits, from a uniform per row: drafts from the diffusion view's logits, tokens of plain
+ * autoregressive decoding from the AR view's.  For row r with x = logits[r][0 .. vocab):
+ *   w_v = exp((x_v - max x) / temperature[r])
+ *   order the tokens by x falling, equal ones by id rising, and keep
+ *     the first top_k[r]                                         (top_k NULL, or <= 0: all)
+ *     of these the shortest stretch from the first whose mass is at least top_p[r] times theirs
+ *                                                                (top_p NULL, NaN, or >= 1: all; <= 0: the first)
+ *     of these the ones with w_v >= min_p[r]                     (min_p NULL, NaN, or <= 0: all)
+ *   the first token always stays;
+ *   token[r] = the first in that order whose running mass exceeds u[r] times the mass kept (u is clamped to [0, 1));
+ *   logprob[r] = log of the token's share of the mass kept (logprob may be NULL).
+ * temperature <= 0 or NaN is greedy: the first token in that order, logprob 0.  NaN and -inf logits are never drawn;
+ * if the largest is +inf, all +inf have equal weight and the others none; a row with nothing to draw from gives token
+ * 0 and logprob NaN.  Weights are taken in double precision and summed as integers (steps of 2^-62 times the vocabulary,
+ * rounded up to a power of two): results do not depend on any order of execution, and differ from an exact evaluation only
+ * where a running mass is within such steps of a border.
+ *   logits  device [rows] rows of `vocab` elements, `row_stride` elements apart (>= vocab), bf16 or fp32
+ *   temperature, top_p, min_p, u, logprob  device float [rows];  top_k, token  device int32 [rows]
+ * 1 <= rows <= 2^20, 1 <= vocab <= 2^24.  No workspace.  One launch.
+ */
+orthrus_status_t orthrus_sample_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+        const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, const float *u,
+        int32_t *token, float *logprob, void *stream);
 
 /*
  * Copies the device status word to *host_status and waits for the stream (the

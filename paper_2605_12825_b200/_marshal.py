@@ -120,3 +120,104 @@ def commit_len(layer, n_commit, workspace, stream):
 def rope_block_kv_write(layer, q, k, v, rope_theta, q_out, workspace, stream):
     _call("orthrus_rope_block_kv_write", ctypes.byref(layer), _ptr(q), _ptr(k), _ptr(v), float(rope_theta), _ptr(q_out),
           _ptr(workspace), _count(workspace), _stream(stream))
+
+
+def _paged(t, name, dtype, shape, optional=False):
+    """A tensor of a paged call: type, shape (None: any size), contiguous, on the current device; its address."""
+    if t is None:
+        if optional:
+            return None
+        raise TypeError(f"{name}: expected a torch tensor")
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: wrong dtype {t.dtype}")
+    if t.dim() != len(shape) or any(w >= 0 and n != w for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{name}: wrong shape {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: not on the current device")
+    return t.data_ptr()
+
+
+def _space(t):
+    if t is None:
+        return None, 0
+    return _paged(t, "workspace", torch.uint8, (-1,)), t.numel()
+
+
+def _rows(layer):
+    return torch.float32 if layer.dtype else torch.bfloat16
+
+
+def page_tables(page_size, cache_len, n_new, held_in, held_out, block_table, free_list, n_free_in, n_free_out, granted, slot_map,
+                workspace, stream):
+    i32 = torch.int32
+    table = _paged(block_table, "block_table", i32, (-1, -1))
+    B, width = block_table.shape
+    per = [_paged(t, n, i32, (B,)) for t, n in ((cache_len, "cache_len"), (n_new, "n_new"), (held_in, "held_in"),
+                                                (held_out, "held_out"))]
+    free = _paged(free_list, "free_list", i32, (-1,))
+    ends = [_paged(n_free_in, "n_free_in", i32, (1,)), _paged(n_free_out, "n_free_out", i32, (1,))]
+    got = _paged(granted, "granted", i32, (B,))
+    slots = _paged(slot_map, "slot_map", torch.int64, (B, -1))
+    _call("orthrus_page_tables", B, page_size, free_list.shape[0], width, slot_map.shape[1], *per, table, free, *ends, got, slots,
+          *_space(workspace), _stream(stream))
+
+
+def _blocks(layer, q, q_out, k, v, slot_map):
+    L, dt = layer, _rows(layer)
+    qs, ks = (L.batch, L.block, L.n_q_heads, L.head_dim), (L.batch, L.block, L.n_kv_heads, L.head_dim)
+    _paged(slot_map, "slot_map", torch.int64, (L.batch, L.block))
+    for t, n, s in ((q, "q", qs), (k, "k_blk", ks), (v, "v_blk", ks), (q_out, "q_out", qs)):
+        if t is not False:
+            _paged(t, n, dt, s)
+
+
+def paged_kv_write(layer, slot_map, k, v, workspace, stream):
+    _blocks(layer, False, False, k, v, slot_map)
+    _call("orthrus_paged_kv_write", ctypes.byref(layer), _ptr(slot_map), _ptr(k), _ptr(v), *_space(workspace), _stream(stream))
+
+
+def rope_paged_kv_write(layer, slot_map, q, k, v, rope_theta, q_out, workspace, stream):
+    _blocks(layer, q, q_out, k, v, slot_map)
+    _call("orthrus_rope_paged_kv_write", ctypes.byref(layer), _ptr(slot_map), _ptr(q), _ptr(k), _ptr(v), float(rope_theta),
+          _ptr(q_out), *_space(workspace), _stream(stream))
+
+
+def paged_commit_len(layer, n_commit, workspace, stream):
+    _call("orthrus_paged_commit_len", ctypes.byref(layer), _paged(n_commit, "n_commit", torch.int32, (layer.batch,)),
+          *_space(workspace), _stream(stream))
+
+
+def _paged_attend(name, layer, q, out, workspace, stream):
+    shape = (layer.batch, layer.block, layer.n_q_heads, layer.head_dim)
+    qp, op = _paged(q, "q", _rows(layer), shape), _paged(out, "out", _rows(layer), shape)
+    _call(name, ctypes.byref(layer), qp, op, *_space(workspace), _stream(stream))
+
+
+def paged_ar_attend(*args):
+    _paged_attend("orthrus_paged_ar_attend", *args)
+
+
+def paged_diffusion_attend(*args):
+    _paged_attend("orthrus_paged_diffusion_attend", *args)
+
+
+def sample_tokens(logits, temperature, top_k, top_p, min_p, u, token, logprob, stream):
+    R, V = _dims(logits, 2)
+    dt = _dtype(logits)
+    if not logits.is_cuda or logits.device.index != torch.cuda.current_device():
+        raise ValueError("logits: expected a CUDA tensor on the current device")
+    if (V > 1 and logits.stride(1) != 1) or (R > 1 and logits.stride(0) < V):
+        raise ValueError("logits: expected rows of neighbouring elements that do not overlap")
+    f32, i32 = torch.float32, torch.int32
+    t, up = _paged(temperature, "temperature", f32, (R,)), _paged(u, "u", f32, (R,))
+    k, p = _paged(top_k, "top_k", i32, (R,), True), _paged(top_p, "top_p", f32, (R,), True)
+    m, tok, lp = (_paged(min_p, "min_p", f32, (R,), True), _paged(token, "token", i32, (R,)),
+                  _paged(logprob, "logprob", f32, (R,), True))
+    _call("orthrus_sample_tokens", logits.data_ptr(), dt, R, V, logits.stride(0) if R > 1 else V, t, k, p, m, up, tok, lp,
+          _stream(stream))

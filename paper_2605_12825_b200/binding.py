@@ -25,7 +25,7 @@ LIB_PATH = os.path.join(_HERE, "liborthrus.so")
 OK = 0
 ERR_TIMEOUT = 6
 BF16, FP32 = 0, 1
-DEV_BAD_CACHE_LEN, DEV_APPEND_OVERFLOW, DEV_WAIT_TIMEOUT = 1, 2, 4
+DEV_BAD_CACHE_LEN, DEV_APPEND_OVERFLOW, DEV_WAIT_TIMEOUT, DEV_NO_PAGES, DEV_BAD_PAGE = 1, 2, 4, 8, 16
 
 EXPORTS = [
     "orthrus_attend_workspace_bytes", "orthrus_workspace_init",
@@ -36,7 +36,9 @@ EXPORTS = [
     "orthrus_consensus_sample",
     "orthrus_lm_head_consensus_workspace_bytes", "orthrus_lm_head_consensus",
     "orthrus_kv_append", "orthrus_kv_append_layers", "orthrus_block_kv_write", "orthrus_commit_len",
-    "orthrus_rope_block_kv_write", "orthrus_read_status", "orthrus_set_path", "orthrus_last_path",
+    "orthrus_rope_block_kv_write", "orthrus_page_tables", "orthrus_paged_kv_write", "orthrus_rope_paged_kv_write",
+    "orthrus_paged_commit_len", "orthrus_paged_attend_workspace_bytes", "orthrus_paged_ar_attend",
+    "orthrus_paged_diffusion_attend", "orthrus_sample_tokens", "orthrus_read_status", "orthrus_set_path", "orthrus_last_path",
     "orthrus_launch_count", "orthrus_status_string", "orthrus_version",
 ]
 
@@ -57,6 +59,16 @@ class Layer(ctypes.Structure):
                 ("v_cache", ctypes.c_void_p), ("cache_len", ctypes.c_void_p),
                 ("max_len_hint", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("flags", ctypes.c_uint32)]
+
+
+class PagedLayer(ctypes.Structure):
+    """Mirror of orthrus_paged_layer_t."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+                ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("cache_len", ctypes.c_void_p), ("n_new", ctypes.c_void_p), ("max_len_hint", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 LAYER_CACHE_QUIESCENT, LAYER_NO_EARLY_LAUNCH, LAYER_BLOCK_IN_CACHE = 1, 2, 4
@@ -108,6 +120,23 @@ def _load() -> ctypes.CDLL:
     lib.orthrus_commit_len.argtypes = [LP, vp, vp, sz, vp]
     lib.orthrus_rope_block_kv_write.restype = ctypes.c_int
     lib.orthrus_rope_block_kv_write.argtypes = [LP, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+    PP = ctypes.POINTER(PagedLayer)
+    lib.orthrus_page_tables.restype = ctypes.c_int
+    lib.orthrus_page_tables.argtypes = [i32] * 5 + [vp] * 10 + [vp, sz, vp]
+    lib.orthrus_paged_kv_write.restype = ctypes.c_int
+    lib.orthrus_paged_kv_write.argtypes = [PP, vp, vp, vp, vp, sz, vp]
+    lib.orthrus_rope_paged_kv_write.restype = ctypes.c_int
+    lib.orthrus_rope_paged_kv_write.argtypes = [PP, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+    lib.orthrus_paged_commit_len.restype = ctypes.c_int
+    lib.orthrus_paged_commit_len.argtypes = [PP, vp, vp, sz, vp]
+    lib.orthrus_paged_attend_workspace_bytes.restype = sz
+    lib.orthrus_paged_attend_workspace_bytes.argtypes = [PP]
+    for name in ("orthrus_paged_ar_attend", "orthrus_paged_diffusion_attend"):
+        f = getattr(lib, name)
+        f.restype = ctypes.c_int
+        f.argtypes = [PP, vp, vp, vp, sz, vp]
+    lib.orthrus_sample_tokens.restype = ctypes.c_int
+    lib.orthrus_sample_tokens.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.orthrus_read_status.restype = ctypes.c_int
     lib.orthrus_read_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     lib.orthrus_set_path.restype = ctypes.c_int
@@ -289,6 +318,91 @@ def orthrus_rope_block_kv_write(layer: Layer, q, k_blk, v_blk, rope_theta: float
     """Rotary embedding of the block's queries (to q_out) and keys, keys and values written to
     cache rows [P_b, P_b + K)."""
     _native.rope_block_kv_write(layer, q, k_blk, v_blk, rope_theta, q_out, workspace, stream)
+
+
+def _device_tensor(t, name: str, dtype, shape, optional: bool = False) -> None:
+    """What the paged calls ask of a tensor: its type, its shape (None: any size), contiguous, on the current CUDA device."""
+    if t is None and optional:
+        return
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{name}: expected shape {tuple('*' if w is None else w for w in shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def make_paged_layer(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, cache_len: torch.Tensor,
+                     n_q_heads: int, block: int, n_new: Optional[torch.Tensor] = None, max_len_hint: int = 0,
+                     softmax_scale: float = 0.0, flags: int = 0) -> PagedLayer:
+    """Describe one layer's pool of pages ([n_pages][Hkv][page_size][d]), the requests' tables ([B][max_pages] int32) and
+    lengths ([B] int32), and the block: `n_new` ([B] int32) rows of each request's `block` exist, all where it is None."""
+    if k_pages.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {k_pages.dtype}")
+    if k_pages.dim() != 4:
+        raise ValueError(f"k_pages: expected [n_pages][Hkv][page_size][d], got {tuple(k_pages.shape)}")
+    n_pages, Hkv, page, d = k_pages.shape
+    _device_tensor(k_pages, "k_pages", k_pages.dtype, k_pages.shape)
+    _device_tensor(v_pages, "v_pages", k_pages.dtype, k_pages.shape)
+    _device_tensor(block_table, "block_table", torch.int32, (None, None))
+    B, width = block_table.shape
+    _device_tensor(cache_len, "cache_len", torch.int32, (B,))
+    _device_tensor(n_new, "n_new", torch.int32, (B,), True)
+    layer = PagedLayer(B, n_q_heads, Hkv, d, block, dtype_code(k_pages.dtype), page, width, n_pages, k_pages.data_ptr(),
+                       v_pages.data_ptr(), block_table.data_ptr(), cache_len.data_ptr(),
+                       None if n_new is None else n_new.data_ptr(), max_len_hint, softmax_scale, flags)
+    layer.tensors = (k_pages, v_pages, block_table, cache_len, n_new)      # alive as long as the descriptor
+    return layer
+
+
+def orthrus_page_tables(page_size: int, cache_len, n_new, held_in, held_out, block_table, free_list, n_free_in, n_free_out,
+                        granted, slot_map, workspace=None, stream=None) -> None:
+    """Pages for the rows that every request adds, taken from and given back to `free_list`, and the slots of these rows;
+    `held_out` may be `held_in` and `n_free_out` may be `n_free_in`."""
+    _native.page_tables(page_size, cache_len, n_new, held_in, held_out, block_table, free_list, n_free_in, n_free_out, granted,
+                        slot_map, workspace, stream)
+
+
+def orthrus_paged_kv_write(layer: PagedLayer, slot_map, k_blk, v_blk, workspace=None, stream=None) -> None:
+    """Block rows [B][K][Hkv][d] to their slots ([B][K] int64, -1: no row)."""
+    _native.paged_kv_write(layer, slot_map, k_blk, v_blk, workspace, stream)
+
+
+def orthrus_rope_paged_kv_write(layer: PagedLayer, slot_map, q, k_blk, v_blk, rope_theta: float, q_out, workspace=None,
+                                stream=None) -> None:
+    """Rotary embedding of the block's queries (to q_out) and keys, keys and values written to their slots."""
+    _native.rope_paged_kv_write(layer, slot_map, q, k_blk, v_blk, rope_theta, q_out, workspace, stream)
+
+
+def orthrus_paged_commit_len(layer: PagedLayer, n_commit, workspace=None, stream=None) -> None:
+    """cache_len += n_commit for the layer's length array."""
+    _native.paged_commit_len(layer, n_commit, workspace, stream)
+
+
+def orthrus_paged_attend_workspace_bytes(layer: PagedLayer) -> int:
+    return int(_lib.orthrus_paged_attend_workspace_bytes(ctypes.byref(layer)))
+
+
+def orthrus_paged_ar_attend(layer: PagedLayer, q, out, workspace, stream=None) -> None:
+    """Causal attention of the rows [B][K][Hq][d] that were written last over their request's pages (K = 1: a decoding step)."""
+    _native.paged_ar_attend(layer, q, out, workspace, stream)
+
+
+def orthrus_paged_diffusion_attend(layer: PagedLayer, q, out, workspace, stream=None) -> None:
+    """The same with a bidirectional block."""
+    _native.paged_diffusion_attend(layer, q, out, workspace, stream)
+
+
+def orthrus_sample_tokens(logits, temperature, top_k, top_p, min_p, u, token, logprob=None, stream=None) -> None:
+    """A token (and the log of its share) per row of logits [R][V], whose rows may be strided; settings and uniforms per row
+    (float32 [R], top_k int32 [R]); top_k, top_p and min_p may be None."""
+    _native.sample_tokens(logits, temperature, top_k, top_p, min_p, u, token, logprob, stream)
 
 
 def orthrus_read_status(workspace, stream=None) -> int:

@@ -35,6 +35,9 @@ static int current_path()
     return v;
 }
 
+bool simt_forced() { return current_path() == PATH_SIMT; }
+void set_last_path(const char *name) { t_last_path = name; }
+
 // The tuning variables of the environment, read at every call that plans (a test changes them
 // between calls).  One walk over the environment, which hardly ever holds any of them, instead of a
 // search per variable: half a dozen searches were a tenth of a call's host time.

@@ -313,6 +313,166 @@ PyObject *rope_block_kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- the paged calls check their tensors: type, shape (below 0: any size), contiguous, on the current device
+void *paged(PyObject *o, const char *name, at::ScalarType type, std::initializer_list<int64_t> shape, bool optional = false)
+{
+    if (o == Py_None && optional) return nullptr;
+    const at::Tensor *t = as_tensor(o);
+    if (!t) { PyErr_Format(PyExc_TypeError, "%s: expected a torch tensor", name); throw Failed(); }
+    if (t->scalar_type() != type) {
+        PyErr_Format(PyExc_TypeError, "%s: wrong dtype %s", name, c10::toString(t->scalar_type()));
+        throw Failed();
+    }
+    bool ok = t->dim() == (int64_t)shape.size();
+    int64_t k = 0;
+    for (int64_t w : shape) { ok = ok && (w < 0 || t->size(k) == w); ++k; }
+    if (!ok) { PyErr_Format(PyExc_ValueError, "%s: wrong shape", name); throw Failed(); }
+    if (!t->is_contiguous()) { PyErr_Format(PyExc_ValueError, "%s: expected a contiguous tensor", name); throw Failed(); }
+    if (!t->is_cuda()) { PyErr_Format(PyExc_ValueError, "%s: expected a CUDA tensor", name); throw Failed(); }
+    if (t->get_device() != c10::cuda::current_device()) {
+        PyErr_Format(PyExc_ValueError, "%s: not on the current device", name);
+        throw Failed();
+    }
+    return t->data_ptr();
+}
+struct Space { void *p; size_t n; };
+Space space_of(PyObject *o)
+{
+    return Space{paged(o, "workspace", at::kByte, {-1}, true), o == Py_None ? 0 : count(o)};
+}
+orthrus_paged_layer_t paged_layer_of(PyObject *o)
+{
+    Py_buffer view;
+    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Failed();
+    if (view.len != (Py_ssize_t)sizeof(orthrus_paged_layer_t)) {
+        PyBuffer_Release(&view);
+        PyErr_SetString(PyExc_TypeError, "expected a PagedLayer");
+        throw Failed();
+    }
+    const orthrus_paged_layer_t L = *static_cast<const orthrus_paged_layer_t *>(view.buf);
+    PyBuffer_Release(&view);
+    return L;
+}
+at::ScalarType type_of(const orthrus_paged_layer_t &L) { return L.dtype == ORTHRUS_FP32 ? at::kFloat : at::kBFloat16; }
+int32_t whole(PyObject *o)
+{
+    const long x = PyLong_AsLong(o);
+    if (x == -1 && PyErr_Occurred()) throw Failed();
+    if (x < INT32_MIN || x > INT32_MAX) { PyErr_SetString(PyExc_ValueError, "a number out of range"); throw Failed(); }
+    return (int32_t)x;
+}
+int32_t extent(const at::Tensor &t, int64_t k)
+{
+    if (t.size(k) > INT32_MAX) { PyErr_SetString(PyExc_ValueError, "a tensor that is too large"); throw Failed(); }
+    return (int32_t)t.size(k);
+}
+
+PyObject *page_tables(PyObject *, PyObject *const *a, Py_ssize_t n)
+{   // page_size, cache_len, n_new, held_in, held_out, block_table, free_list, n_free_in, n_free_out, granted, slot_map, workspace, stream
+    const char *name = "orthrus_page_tables";
+    return guarded(n, 13, name, [&]() -> PyObject * {
+        const int32_t page = whole(a[0]);
+        auto i32 = [&](int k, const char *what, std::initializer_list<int64_t> s) { return static_cast<int32_t *>(paged(a[k], what, at::kInt, s)); };
+        int32_t *table = i32(5, "block_table", {-1, -1});
+        const int32_t B = extent(*as_tensor(a[5]), 0), W = extent(*as_tensor(a[5]), 1);
+        int32_t *len = i32(1, "cache_len", {B}), *add = i32(2, "n_new", {B}), *hi = i32(3, "held_in", {B}), *ho = i32(4, "held_out", {B});
+        int32_t *fl = i32(6, "free_list", {-1}), *fi = i32(7, "n_free_in", {1}), *fo = i32(8, "n_free_out", {1}), *gr = i32(9, "granted", {B});
+        int64_t *sm = static_cast<int64_t *>(paged(a[10], "slot_map", at::kLong, {B, -1}));
+        const int32_t N = extent(*as_tensor(a[6]), 0), M = extent(*as_tensor(a[10]), 1);
+        const Space ws = space_of(a[11]);
+        void *st = stream_of(a[12]);
+        return finish(name, [&] { return orthrus_page_tables(B, page, N, W, M, len, add, hi, ho, table, fl, fi, fo, gr, sm, ws.p, ws.n, st); });
+    });
+}
+
+PyObject *paged_kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{   // layer, slot_map, k_blk, v_blk, workspace, stream
+    const char *name = "orthrus_paged_kv_write";
+    return guarded(n, 6, name, [&]() -> PyObject * {
+        const orthrus_paged_layer_t L = paged_layer_of(a[0]);
+        const int64_t *sm = static_cast<int64_t *>(paged(a[1], "slot_map", at::kLong, {L.batch, L.block}));
+        void *k = paged(a[2], "k_blk", type_of(L), {L.batch, L.block, L.n_kv_heads, L.head_dim});
+        void *v = paged(a[3], "v_blk", type_of(L), {L.batch, L.block, L.n_kv_heads, L.head_dim});
+        const Space ws = space_of(a[4]);
+        void *st = stream_of(a[5]);
+        return finish(name, [&] { return orthrus_paged_kv_write(&L, sm, k, v, ws.p, ws.n, st); });
+    });
+}
+
+PyObject *rope_paged_kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{   // layer, slot_map, q, k_blk, v_blk, rope_theta, q_out, workspace, stream
+    const char *name = "orthrus_rope_paged_kv_write";
+    return guarded(n, 9, name, [&]() -> PyObject * {
+        const orthrus_paged_layer_t L = paged_layer_of(a[0]);
+        const int64_t *sm = static_cast<int64_t *>(paged(a[1], "slot_map", at::kLong, {L.batch, L.block}));
+        void *q = paged(a[2], "q", type_of(L), {L.batch, L.block, L.n_q_heads, L.head_dim});
+        void *k = paged(a[3], "k_blk", type_of(L), {L.batch, L.block, L.n_kv_heads, L.head_dim});
+        void *v = paged(a[4], "v_blk", type_of(L), {L.batch, L.block, L.n_kv_heads, L.head_dim});
+        const float theta = (float)real(a[5]);
+        void *qo = paged(a[6], "q_out", type_of(L), {L.batch, L.block, L.n_q_heads, L.head_dim});
+        const Space ws = space_of(a[7]);
+        void *st = stream_of(a[8]);
+        return finish(name, [&] { return orthrus_rope_paged_kv_write(&L, sm, q, k, v, theta, qo, ws.p, ws.n, st); });
+    });
+}
+
+PyObject *paged_commit_len(PyObject *, PyObject *const *a, Py_ssize_t n)
+{   // layer, n_commit, workspace, stream
+    const char *name = "orthrus_paged_commit_len";
+    return guarded(n, 4, name, [&]() -> PyObject * {
+        const orthrus_paged_layer_t L = paged_layer_of(a[0]);
+        const int32_t *nc = static_cast<int32_t *>(paged(a[1], "n_commit", at::kInt, {L.batch}));
+        const Space ws = space_of(a[2]);
+        void *st = stream_of(a[3]);
+        return finish(name, [&] { return orthrus_paged_commit_len(&L, nc, ws.p, ws.n, st); });
+    });
+}
+
+template <class Fn> PyObject *paged_attend(PyObject *const *a, Py_ssize_t n, const char *name, Fn fn)
+{   // layer, q, out, workspace, stream
+    return guarded(n, 5, name, [&]() -> PyObject * {
+        const orthrus_paged_layer_t L = paged_layer_of(a[0]);
+        void *q = paged(a[1], "q", type_of(L), {L.batch, L.block, L.n_q_heads, L.head_dim});
+        void *out = paged(a[2], "out", type_of(L), {L.batch, L.block, L.n_q_heads, L.head_dim});
+        const Space ws = space_of(a[3]);
+        void *st = stream_of(a[4]);
+        return finish(name, [&] { return fn(&L, q, out, ws.p, ws.n, st); });
+    });
+}
+PyObject *paged_ar_attend(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return paged_attend(a, n, "orthrus_paged_ar_attend", orthrus_paged_ar_attend);
+}
+PyObject *paged_diffusion_attend(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return paged_attend(a, n, "orthrus_paged_diffusion_attend", orthrus_paged_diffusion_attend);
+}
+
+PyObject *sample_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
+{   // logits, temperature, top_k, top_p, min_p, u, token, logprob, stream
+    const char *name = "orthrus_sample_tokens";
+    return guarded(n, 9, name, [&]() -> PyObject * {
+        const at::Tensor &x = need_tensor(a[0], 2);
+        const int32_t R = extent(x, 0), V = extent(x, 1), dt = dtype_of(x);
+        if (!x.is_cuda() || x.get_device() != c10::cuda::current_device()) {
+            PyErr_SetString(PyExc_ValueError, "logits: expected a CUDA tensor on the current device");
+            throw Failed();
+        }
+        if ((V > 1 && x.stride(1) != 1) || (R > 1 && x.stride(0) < V)) {
+            PyErr_SetString(PyExc_ValueError, "logits: expected rows of neighbouring elements that do not overlap");
+            throw Failed();
+        }
+        auto f32 = [&](int k, const char *what, bool optional) { return static_cast<float *>(paged(a[k], what, at::kFloat, {R}, optional)); };
+        const float *t = f32(1, "temperature", false), *p = f32(3, "top_p", true), *m = f32(4, "min_p", true), *u = f32(5, "u", false);
+        const int32_t *k = static_cast<int32_t *>(paged(a[2], "top_k", at::kInt, {R}, true));
+        int32_t *tok = static_cast<int32_t *>(paged(a[6], "token", at::kInt, {R}));
+        float *lp = f32(7, "logprob", true);
+        void *lg = x.data_ptr(), *st = stream_of(a[8]);
+        const int64_t stride = R > 1 ? x.stride(0) : V;
+        return finish(name, [&] { return orthrus_sample_tokens(lg, dt, R, V, stride, t, k, p, m, u, tok, lp, st); });
+    });
+}
+
 PyObject *set_raiser(PyObject *, PyObject *f)
 {
     Py_XINCREF(f);
@@ -325,6 +485,8 @@ PyMethodDef methods[] = {
     FAST(diffusion_block_attend), FAST(ar_verify_attend), FAST(multi_block_attend), FAST(consensus_accept),
     FAST(consensus_accept_static), FAST(consensus_sample), FAST(lm_head_consensus), FAST(kv_append),
     FAST(kv_append_layers), FAST(block_kv_write), FAST(commit_len), FAST(rope_block_kv_write),
+    FAST(page_tables), FAST(paged_kv_write), FAST(rope_paged_kv_write), FAST(paged_commit_len), FAST(paged_ar_attend),
+    FAST(paged_diffusion_attend), FAST(sample_tokens),
     {"set_raiser", set_raiser, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,154 @@
+// Block tables and slot maps from the requests' lengths, in one launch.
+//
+// need = ceil((len + new) / page); a request gives back held - need pages or takes need - held.  Where its pages lie in the
+// list of free ones follows from two sums over the requests before it, so that every result is fixed by the inputs:
+//   given back   free_list[n_free + (given by requests before) + k]             k = 0, 1, .. in page order
+//   taken        free_list[total - 1 - (taken by requests before) - k]          total = n_free + all that is given back
+// One cluster: every CTA works out both sums for all requests (a block scan; a few KB from L2), gives back its share of the
+// pages, meets the others at the cluster's barrier, and then hands out and maps its share: two phases in one launch, where two
+// launches would read the lengths twice and wait for one another through the stream.  The barrier also stands between the last read of
+// held_in and n_free_in and the first write of their successors, which may be the same arrays.
+//
+// What bounds it: latency (lengths, scan, barrier, list, table: five dependent steps) for a decoding batch; for prompts the 8 bytes
+// a slot, which the CTAs of the cluster write.
+#include "paged.cuh"
+#include "tc_ptx.cuh"
+
+namespace orthrus {
+namespace {
+
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kStretch = 256;                    // slots a warp maps at a time
+
+struct Entry { uint32_t gives, takes; int need, held; };       // sums before / up to and with the request; need < 0: left alone
+
+__device__ inline unsigned long long warp_scan(unsigned long long x, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const unsigned long long y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+    }
+    return x;
+}
+
+__global__ void __launch_bounds__(kThreads, 1) page_tables_kernel(const PageTablesParams p, int per)
+{
+    extern __shared__ Entry entry[];
+    __shared__ unsigned long long sum[2][kWarps];
+    __shared__ unsigned upto;                    // pages taken by the requests that are served
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = gridDim.x, rank = blockIdx.x;
+    if (tid == 0) upto = 0;
+    pdl_begin();
+
+    // sums over the requests: a thread's own `per` ones, then the block's
+    unsigned long long g = 0, t = 0;
+    int flags = 0;
+    const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
+    for (int b = b0; b < b1; ++b) {
+        const int len = p.cache_len[b], add = p.n_new[b], held = p.held_in[b];
+        const long long need = ((long long)len + add + (1 << p.page_shift) - 1) >> p.page_shift;
+        const bool ok = len >= 0 && add >= 0 && add <= p.max_new && held >= 0 && held <= p.max_pages && need <= p.max_pages;
+        if (!ok) flags |= ORTHRUS_DEV_BAD_CACHE_LEN;
+        entry[b] = Entry{0, 0, ok ? (int)need : -1, held};
+        if (ok && need < held) g += held - need;
+        if (ok && need > held) t += need - held;
+    }
+    unsigned long long gs = warp_scan(g, lane), ts = warp_scan(t, lane);
+    if (lane == 31) { sum[0][warp] = gs; sum[1][warp] = ts; }
+    __syncthreads();
+    if (warp < 2) sum[warp][lane] = warp_scan(sum[warp][lane], lane);
+    __syncthreads();
+    gs += (warp ? sum[0][warp - 1] : 0) - g;
+    ts += (warp ? sum[1][warp - 1] : 0) - t;
+    const unsigned long long given = sum[0][kWarps - 1];
+    int n_free = *p.n_free_in;
+    if (n_free < 0 || n_free > p.n_pages || given > (unsigned long long)(p.n_pages - n_free)) flags |= ORTHRUS_DEV_NO_PAGES;
+    n_free = min(max(n_free, 0), p.n_pages);
+    const unsigned total = (unsigned)min((unsigned long long)p.n_pages, n_free + given);
+    unsigned most = 0;
+    for (int b = b0; b < b1; ++b) {
+        Entry e = entry[b];
+        const int change = e.need < 0 ? 0 : e.need - e.held;
+        if (change > 0) ts += change;
+        e.gives = (uint32_t)min(gs, 0xffffffffull);
+        e.takes = (uint32_t)min(ts, 0xffffffffull);
+        if (change < 0) gs -= change;
+        if (change > 0) {
+            if (e.takes <= total) most = e.takes;
+            else { e.need = -2; flags |= ORTHRUS_DEV_NO_PAGES; }        // not served
+        }
+        entry[b] = e;
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0 && most) atomicMax(&upto, most);
+    flags = __reduce_or_sync(0xffffffffu, (unsigned)flags);
+    if (flags && lane == 0 && rank == 0 && p.status) atomicOr(p.status, flags);
+    __syncthreads();
+
+    // pages that are given back
+    const int first = rank * kWarps + warp, stride = C * kWarps;
+    for (int b = first; b < p.B; b += stride) {
+        const Entry e = entry[b];
+        if (e.need < 0) continue;
+        for (int j = e.need + lane; j < e.held; j += 32) {
+            const unsigned long long at = (unsigned long long)n_free + e.gives + (j - e.need);
+            if (at < (unsigned long long)p.n_pages) p.free_list[at] = p.table[(long long)b * p.max_pages + j];
+        }
+    }
+    cluster_sync_all();
+
+    // pages that are taken
+    auto taken = [&](const Entry &e, int j) {                  // page j >= held of a request that is served
+        return __ldcg(p.free_list + (total - 1 - (e.takes - (unsigned)(e.need - e.held) + (unsigned)(j - e.held))));
+    };
+    for (int b = first; b < p.B; b += stride) {
+        const Entry e = entry[b];
+        for (int j = e.held + lane; j < e.need; j += 32) p.table[(long long)b * p.max_pages + j] = taken(e, j);
+    }
+    // slots: a stretch of a request's rows at a time
+    const int stretches = (p.max_new + kStretch - 1) / kStretch;
+    for (long long it = first; it < (long long)p.B * stretches; it += stride) {
+        const int b = (int)(it / stretches), i0 = (int)(it - (long long)b * stretches) * kStretch;
+        const Entry e = entry[b];
+        const int len = p.cache_len[b], n = e.need < 0 ? 0 : p.n_new[b];
+        int64_t *out = p.slot_map + (long long)b * p.max_new;
+        const int32_t *mine = p.table + (long long)b * p.max_pages;
+#pragma unroll
+        for (int k = 0; k < kStretch / 32; ++k) {
+            const int i = i0 + k * 32 + lane;
+            if (i >= p.max_new) break;
+            long long slot = -1;
+            if (i < n) {
+                const int pos = len + i, j = pos >> p.page_shift;
+                const long long page = j < e.held ? mine[j] : taken(e, j);
+                slot = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+            }
+            out[i] = slot;
+        }
+    }
+    for (int b = rank * kThreads + tid; b < p.B; b += C * kThreads) {
+        const Entry e = entry[b];
+        p.granted[b] = e.need < 0 ? 0 : p.n_new[b];
+        p.held_out[b] = e.need < 0 ? e.held : e.need;
+    }
+    if (rank == 0 && tid == 0) *p.n_free_out = (int)(total - upto);
+}
+
+}  // namespace
+
+cudaError_t launch_page_tables(const PageTablesParams &p, cudaStream_t st)
+{
+    // CTAs by the slots to write
+    const long long slots = (long long)p.B * ((p.max_new + 31) / 32 * 32);
+    int C = slots <= 8192 ? 1 : slots <= 32768 ? 4 : 8;
+    if (slots > 131072 && clusters_resident(16, 1) > 0) C = 16;
+    static std::atomic<uint64_t> done{0};
+    const int smem = p.B * (int)sizeof(Entry);
+    const cudaError_t e = configure(page_tables_kernel, done, 8192 * (int)sizeof(Entry), true);
+    if (e != cudaSuccess) return e;
+    return launch_clusters(true, C, page_tables_kernel, dim3(C), kThreads, smem, st, p, (p.B + kThreads - 1) / kThreads);
+}
+
+}  // namespace orthrus

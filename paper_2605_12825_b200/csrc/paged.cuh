@@ -1,0 +1,94 @@
+// Declarations of the paged-cache calls: what their translation units share.
+#pragma once
+#include <atomic>
+#include "common.cuh"
+
+namespace orthrus {
+
+struct PageTablesParams {
+    int B, page_shift, n_pages, max_pages, max_new;
+    const int32_t *cache_len, *n_new, *held_in;
+    int32_t *held_out, *table, *free_list;
+    const int32_t *n_free_in;
+    int32_t *n_free_out, *granted;
+    int64_t *slot_map;
+    int32_t *status;
+};
+cudaError_t launch_page_tables(const PageTablesParams &p, cudaStream_t st);
+
+cudaError_t launch_paged_kv_write(const orthrus_paged_layer_t &L, const int64_t *slot_map, const void *q, const void *k_blk,
+                                  const void *v_blk, double theta, void *q_out, int32_t *status, cudaStream_t st);   // q null: no rotation
+
+// Attention over pages.  A unit is (request, KV head, tile of query rows); rows of a request are ordered
+// r = i * G + g as in AttnParams.
+struct PagedParams {
+    const void *q, *k_pages, *v_pages;
+    const int32_t *table, *cache_len, *n_new;
+    void *out;
+    int32_t *status;
+    int B, K, Hq, Hkv, G, d;
+    int page_shift, max_pages;
+    long long n_pages;
+    int max_pos;            // max_pages * page_size
+    int causal;
+    float scale_log2;
+    int early, quiescent;   // launch as a programmatic dependent; first tiles ahead of the preceding kernel
+};
+bool simt_forced();                         // orthrus_set_path("simt")
+void set_last_path(const char *name);       // what orthrus_last_path() answers on this thread; a literal
+cudaError_t launch_paged_attend_simt(const PagedParams &p, int dtype, cudaStream_t st);
+bool paged_tc_shape(const orthrus_paged_layer_t &L);        // the tensor-core kernel serves this shape
+size_t paged_tc_workspace_bytes(const orthrus_paged_layer_t &L);
+cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_layer_t &L, void *ws_body, cudaStream_t st);
+
+// prefix length and rows of request b, clamped to what the layer can hold (`bad`: they had to be)
+__device__ inline void paged_request(const PagedParams &p, int b, int &P, int &n, bool &bad)
+{
+    P = p.cache_len[b];
+    n = p.n_new ? p.n_new[b] : p.K;
+    bad = n < 0 || n > p.K;
+    n = min(max(n, 0), min(p.K, p.max_pos));
+    bad |= P < 0 || P > p.max_pos - n;
+    P = min(max(P, 0), p.max_pos - n);
+}
+
+cudaError_t launch_sample_tokens(const void *logits, int dtype, int rows, int vocab, long long stride, const float *temperature,
+                                 const int32_t *top_k, const float *top_p, const float *min_p, const float *u, int32_t *token,
+                                 float *logprob, cudaStream_t st);
+
+// launch_kernel in clusters of C CTAs along x
+template <class... Params, class... Args>
+cudaError_t launch_clusters(bool early, int C, void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem,
+                            cudaStream_t st, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = early && early_launch_allowed() ? 2 : 1;
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
+// Attributes of a kernel, set once per device.  `done`: a static of the caller's, one bit per device.
+template <class Kernel>
+cudaError_t configure(Kernel *kernel, std::atomic<uint64_t> &done, int smem, bool wide_clusters)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1)) return cudaSuccess;
+    if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
+    if (wide_clusters && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) done.fetch_or(1ull << dev, std::memory_order_release);
+    return cudaSuccess;
+}
+
+}  // namespace orthrus
