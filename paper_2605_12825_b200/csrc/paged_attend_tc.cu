@@ -1,0 +1,417 @@
+// Attention over the pages of a paged cache for units of more than 16 query rows, bf16, head_dim 64 and 128, on tcgen05: blocks of either
+// view, wide groups.  Work is cut and pieces are joined as in paged_attend_mma.cu (which see); a unit's query tile is 128 rows.
+//
+//   S [128 rows x 64 keys] = Q K^T          O [128 rows x d] += P V,  P = 2^(S scale - reference)
+//
+// What bounds it: HBM up to some 64 rows, then the softmax (64 exponentials a row and tile) and the MMAs.  Rows that a unit does not have
+// are padding of the MMA, but cost no softmax.  CTA of 192 threads, 113 KB of shared memory and 256 TMEM columns: two fit an SM, so that one's
+// softmax overlaps the other's products.
+//   warps 0-3  softmax, thread = query row: scores from tensor memory, probabilities back to it as bf16 in their place; also the
+//              query rows' way into shared memory, the read-out, and the join
+//   warp 4     producer: K and V tiles into a ring of slots, a TMA box per page and 64 columns
+//   warp 5     MMAs: the scores of the next tile are issued ahead of the product of this one
+// A row's reference follows its maximum only when that has grown by more than 2^8 since: the output in tensor memory is rescaled rarely,
+// numerator and denominator use the same reference, and probabilities stay below 2^8.
+// Every wait is bounded: on expiry the CTA raises ORTHRUS_DEV_WAIT_TIMEOUT, waits for its copies and MMAs in flight and ends.
+#include <cuda.h>
+#include "paged_stretch.cuh"
+
+namespace orthrus {
+namespace {
+
+constexpr int MROWS = 128, PRODUCER = 4, MMA = 5, NTHREADS = 192;
+constexpr float kSlack = 8.f;             // log2 of what a probability may be
+
+__device__ inline void bar_softmax() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ inline bool bar_softmax_and(bool ok) {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.and.pred q, 1, 128, p;\n"
+                 " selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"((uint32_t)ok) : "memory");
+    return r != 0;
+}
+
+template <int HD> struct Shape {
+    static constexpr int PANELS = HD / 64, QSUB = MROWS * 128, SUB = KT * 128, SLOT = PANELS * SUB;   // bytes
+    static constexpr int NSLOT = HD == 128 ? 5 : 10;
+    static constexpr int OFF_Q = 0, OFF_RING = PANELS * QSUB, OFF_BAR = OFF_RING + NSLOT * SLOT;
+    // barriers: slots full, slots empty, scores (two buffers), probabilities (two), products done, query rows, drained
+    static constexpr int FULL = 0, EMPTY = NSLOT, SCORES = 2 * NSLOT, PROBS = SCORES + 2, PRODUCT = PROBS + 2, QUERY = PRODUCT + 1,
+                         DRAIN = QUERY + 1, BARS = DRAIN + 1;
+    static constexpr int OFF_MISC = OFF_BAR + BARS * 8, SMEM = OFF_MISC + 16;
+    static constexpr uint32_t TM_S = HD, TM_COLS = 256;            // O, then two buffers of scores
+    // the join: weights of the pieces [piece][row], in the place of the query rows
+    static constexpr int MOST = PANELS * QSUB / (MROWS * 4);
+    static_assert(2 * (SMEM + 1024) <= 228 * 1024 && kMostWide <= MOST, "two CTAs per SM; the join");
+};
+
+template <int HD>
+__global__ void __launch_bounds__(NTHREADS, 2)
+paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedWork w)
+{
+    using C = Shape<HD>;
+    constexpr int NSLOT = C::NSLOT, PANELS = C::PANELS;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t sbase = smem_u32(smem);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::OFF_MISC);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::OFF_MISC + 4);
+    int *last_flag = reinterpret_cast<int *>(smem + C::OFF_MISC + 8);
+    auto bar = [&](int i) { return sbase + C::OFF_BAR + i * 8; };
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (warp == MMA) {
+        if (lane == 0) {
+            *abort_flag = (sbase & 1023u) == 0 ? 0 : 1;      // swizzled tiles need 1 KB alignment
+            for (int i = 0; i < C::BARS; ++i) mbar_init(bar(i), i == C::PROBS || i == C::PROBS + 1 || i == C::QUERY ? 4 : 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            fence_proxy_async();
+        }
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(tmem_slot)), "r"(C::TM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int U = p.Hkv * w.row_tiles, page = 1 << p.page_shift;
+    Stretch s;
+    Piece x;
+    // tile number T of the CTA: K in ring item 2 T, V in 2 T + 1; item j in slot j % NSLOT
+    if (warp == PRODUCER) {
+        // ------------------------------------------------------------------ producer
+        bool waited = false;
+        auto wait = [&] { griddep_wait(); griddep_launch(); waited = true; };
+        if (!p.quiescent) wait();
+        int items = 0;
+        if (lane == 0) { prefetch_map(&tm.k); prefetch_map(&tm.v); }
+        if (find_stretch(p, U, blockIdx.x, gridDim.x, w.most_pieces, lane, blockIdx.x == 0, s)) {
+            const long long start = s.pos;
+            const uint64_t policy = policy_evict_first();
+            const int box = 1 << w.box_shift;
+            bool ok = true;
+            PageWindow pages;
+            while (ok && next_piece(p, s, start, lane, x)) {
+                const int h = x.u / w.row_tiles, keys = x.P + x.n;
+                pages.open(p, x, lane);
+                for (int t = x.t0; ok && t < x.t1; ++t) {
+                    const int pos0 = t * KT;
+                    if (!waited && pos0 + KT > x.P) wait();                                   // rows of the block itself
+                    const int last = min(pos0 + KT, keys) - 1;
+                    const int i = lane & 3, pan = lane >> 2;                                  // lane: box and panel
+                    const int pos = pos0 + (i << w.box_shift), pg = pages.page(p, pos, last, lane);
+                    const int live = ((last - pos0) >> w.box_shift) + 1;
+                    const int row = ((pg * p.Hkv + h) << p.page_shift) + (pos & (page - 1));
+#pragma unroll
+                    for (int kind = 0; kind < 2; ++kind) {
+                        const int slot = items % NSLOT;
+                        if (items >= NSLOT) ok = mbar_wait_warp(bar(C::EMPTY + slot), (items / NSLOT + 1) & 1, abort_flag);
+                        if (!ok) break;
+                        if (lane == 0) mbar_expect_tx(bar(C::FULL + slot), live * box * HD * 2);
+                        __syncwarp();
+                        if (lane < 4 * PANELS && i < live)
+                            tma_load_2d(sbase + C::OFF_RING + slot * C::SLOT + pan * C::SUB + i * (box * 128), kind ? &tm.v : &tm.k, pan * 64, row,
+                                        bar(C::FULL + slot), policy);
+                        __syncwarp();
+                        ++items;
+                    }
+                }
+            }
+        }
+        if (!waited) wait();
+        if (*abort_flag && lane == 0)                   // the last copies, before the block can end
+            for (int k = max(0, items - NSLOT); k < items; ++k) mbar_wait_long(bar(C::FULL + k % NSLOT), (k / NSLOT) & 1);
+        __syncwarp();
+    } else if (warp == MMA) {
+        // ------------------------------------------------------------------ MMAs
+        griddep_wait();
+        constexpr uint32_t IDESC_QK = make_idesc(KT, 0), IDESC_PV = make_idesc(HD, 1);
+        const uint64_t q_desc = make_desc(sbase + C::OFF_Q, 16, 1024);
+        bool ok = find_stretch(p, U, blockIdx.x, gridDim.x, w.most_pieces, lane, false, s);
+        const long long start = ok ? s.pos : 0;
+        int T = 0, units = 0;
+        auto full = [&](int item) { return mbar_wait_warp(bar(C::FULL + item % NSLOT), (item / NSLOT) & 1, abort_flag); };
+        auto scores = [&](int T) {
+            const int slot = 2 * T % NSLOT;
+            if (elect_one()) {
+                const uint64_t kd = make_desc(sbase + C::OFF_RING + slot * C::SLOT, 16, 1024);
+                const uint32_t d = tmem + C::TM_S + (T & 1) * KT;
+#pragma unroll
+                for (int kk = 0; kk < HD / 16; ++kk)
+                    umma_ss(d, q_desc + (((kk >> 2) * C::QSUB + (kk & 3) * 32) >> 4), kd + (((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4), IDESC_QK, kk > 0);
+                umma_commit(bar(C::EMPTY + slot));
+                umma_commit(bar(C::SCORES + (T & 1)));
+            }
+            __syncwarp();
+        };
+        while (ok && next_piece(p, s, start, lane, x)) {
+            const int tiles = x.t1 - x.t0;
+            ok = mbar_wait_warp(bar(C::QUERY), units & 1, abort_flag) && full(2 * T);
+            if (!ok) break;
+            tc_fence_after();
+            scores(T);
+            for (int t = 0; t < tiles; ++t, ++T) {
+                if (t + 1 < tiles) {
+                    ok = full(2 * (T + 1));
+                    if (!ok) break;
+                    scores(T + 1);
+                }
+                ok = mbar_wait_warp(bar(C::PROBS + (T & 1)), (T >> 1) & 1, abort_flag) && full(2 * T + 1);
+                if (!ok) break;
+                tc_fence_after();
+                const int slot = (2 * T + 1) % NSLOT;
+                if (elect_one()) {
+                    const uint64_t vd = make_desc(sbase + C::OFF_RING + slot * C::SLOT, C::SUB, 1024);
+                    const uint32_t a = tmem + C::TM_S + (T & 1) * KT;
+#pragma unroll
+                    for (int kk = 0; kk < KT / 16; ++kk) umma_ts(tmem, a + kk * 8, vd + (kk * 2048 >> 4), IDESC_PV, t > 0 || kk > 0);
+                    umma_commit(bar(C::EMPTY + slot));
+                    umma_commit(bar(C::PRODUCT));
+                }
+                __syncwarp();
+            }
+            ++units;
+        }
+        if (*abort_flag) {                              // the MMAs in flight, before their operands and tensor memory go
+            if (elect_one()) umma_commit(bar(C::DRAIN));
+            __syncwarp();
+            mbar_wait_long(bar(C::DRAIN), 0);
+        }
+    } else {
+        // ------------------------------------------------------------------ softmax
+        griddep_wait();
+        const int r = tid;
+        const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
+        bool ok = find_stretch(p, U, blockIdx.x, gridDim.x, w.most_pieces, lane, false, s);
+        const long long start = ok ? s.pos : 0;
+        int T = 0;
+        while (ok && next_piece(p, s, start, lane, x)) {
+            const int h = x.u / w.row_tiles, r0 = (x.u - h * w.row_tiles) * MROWS, M = x.n * p.G, keys = x.P + x.n;
+            const int rows = max(0, min(MROWS, M - r0));
+            const bool at_work = warp * 32 < rows;       // (other warps have padding only)
+            const long long at = r < rows ? row_offset(p, x.b, h, r0 + r, HD) : 0;
+            // this thread's query row, into swizzled panels of 64 columns; a row that does not exist is left as it is
+            if (r < rows) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + at);
+                uint4 v[HD / 8];
+#pragma unroll
+                for (int c = 0; c < HD / 8; ++c) v[c] = src[c];
+#pragma unroll
+                for (int c = 0; c < HD / 8; ++c)
+                    *reinterpret_cast<uint4 *>(smem + C::OFF_Q + (c >> 3) * C::QSUB + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[c];
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::QUERY));
+            const int sees = p.causal ? min(keys, x.P + (r0 + r) / p.G + 1) : keys;
+            float ref = -INFINITY, l = 0.f;
+            for (int t = x.t0; t < x.t1; ++t, ++T) {
+                const int pos0 = t * KT;
+                const uint32_t ts = mine + C::TM_S + (T & 1) * KT;
+                if (!mbar_wait_warp(bar(C::SCORES + (T & 1)), (T >> 1) & 1, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                if (at_work) {
+                    uint32_t raw[KT];
+                    float sc[KT];
+                    tmem_ld<KT>(ts, raw);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < KT; ++j) sc[j] = __uint_as_float(raw[j]);
+                    if (pos0 + KT > x.P) {               // some keys are the block's own, or do not exist
+#pragma unroll
+                        for (int j = 0; j < KT; ++j) sc[j] = pos0 + j < sees ? sc[j] : -INFINITY;
+                    }
+                    float top = max3(sc[0], sc[1], sc[2]);
+#pragma unroll
+                    for (int j = 3; j + 1 < KT; j += 2) top = max3(top, sc[j], sc[j + 1]);
+                    top = fmaxf(top, sc[KT - 1]) * p.scale_log2;
+                    const bool move = top > ref + kSlack || (ref == -INFINITY && top > -INFINITY);
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float next = move ? top : ref, al = next == -INFINITY ? 1.f : ex2(ref - next);
+                        ref = next;
+                        l *= al;
+                        if (t > x.t0) {
+                            // the products so far, which are the sums up to the tile before
+                            if (!mbar_wait_warp(bar(C::PRODUCT), (T - 1) & 1, abort_flag)) { ok = false; break; }
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < HD; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(mine + c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * al);
+                                tmem_st32(mine + c, o);
+                            }
+                        }
+                    }
+                    const float from = ref == -INFINITY ? 0.f : ref;
+                    uint32_t pk[KT / 2];
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < KT; j += 2) {
+                        const float a = ex2(fmaf(sc[j], p.scale_log2, -from)), b = ex2(fmaf(sc[j + 1], p.scale_log2, -from));
+                        sum[(j >> 1) & 3] += a + b;
+                        pk[j >> 1] = pack_bf16(a, b);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_st32(ts, pk);
+                    tmem_st_wait();
+                }
+                if (pos0 + KT > keys) {
+                    // rows behind the last key, which may hold anything: zero, for the product with their zero probabilities
+                    const int item = 2 * T + 1, slot = item % NSLOT;
+                    if (!mbar_wait_warp(bar(C::FULL + slot), (item / NSLOT) & 1, abort_flag)) { ok = false; break; }
+                    const int n0 = keys - pos0, n = (KT - n0) * (HD / 8);
+                    for (int e = tid; e < n; e += 128) {
+                        const int row = n0 + e / (HD / 8), c = e % (HD / 8);
+                        *reinterpret_cast<uint4 *>(smem + C::OFF_RING + slot * C::SLOT + (c >> 3) * C::SUB + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::PROBS + (T & 1)));
+            }
+            if (ok) ok = mbar_wait_warp(bar(C::PRODUCT), (T - 1) & 1, abort_flag);
+            ok = bar_softmax_and(ok);              // (a warp whose wait ran out has come here too: all leave together)
+            if (!ok) break;
+            tc_fence_after();
+            if (x.t0 == 0 && x.t1 == x.tiles) {
+                if (at_work) {
+                    const float inv = 1.f / l;
+#pragma unroll 1
+                    for (int c = 0; c < HD; c += 32) {
+                        uint32_t raw[32];
+                        float o[32];
+                        tmem_ld32(mine + c, raw);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(raw[j]);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8)
+                            st_global_if(r < rows, static_cast<__nv_bfloat16 *>(p.out) + at + c + j,
+                                         make_uint4(pack_bf16(o[j] * inv, o[j + 1] * inv), pack_bf16(o[j + 2] * inv, o[j + 3] * inv),
+                                                    pack_bf16(o[j + 4] * inv, o[j + 5] * inv), pack_bf16(o[j + 6] * inv, o[j + 7] * inv)));
+                    }
+                    tc_fence_before();
+                }
+                continue;
+            }
+            // a piece: [four columns][row], so that a warp's store is 512 contiguous bytes
+            const size_t step = piece_floats(w.rows, HD), stats = (size_t)w.rows * HD;
+            float *to = w.pieces + (2 * blockIdx.x + (x.first ? 0 : 1)) * step;
+            if (at_work) {
+#pragma unroll 1
+                for (int c = 0; c < HD; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(mine + c, o);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4)
+                        st_global_if(r < rows, to + ((size_t)(c + j) / 4 * w.rows + r) * 4, make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+                }
+                tc_fence_before();
+                if (r < rows) *reinterpret_cast<float2 *>(to + stats + r * 2) = make_float2(ref, l);
+            }
+            const int c0 = owner(s, x.unit0), n = owner(s, x.unit0 + x.tiles - 1) - c0 + 1;
+            bar_softmax();
+            if (tid == 0) {
+                int *counter = w.counter + (long long)x.b * U + x.u;
+                __threadfence();
+                const bool last = atomicAdd(counter, 1) == n - 1;
+                if (last) { *counter = 0; __threadfence(); }
+                *last_flag = last;
+            }
+            bar_softmax();
+            if (!*last_flag || rows == 0) continue;
+            // The join.  Weights first (a thread its row), in the place of the query rows; then `groups` threads share a row's columns.
+            const float *first = w.pieces + (2 * c0 + (s.T * c0 / s.n == x.unit0 ? 0 : 1)) * step, *others = w.pieces + 2 * c0 * step;
+            auto piece = [&](int k) { return k ? others + 2 * k * step : first; };
+            float *wt = reinterpret_cast<float *>(smem + C::OFF_Q);
+            if (r < rows) {
+                float top = -INFINITY, sum = 0.f;
+#pragma unroll 8
+                for (int k = 0; k < n; ++k) {
+                    const float2 st = __ldcg(reinterpret_cast<const float2 *>(piece(k) + stats + r * 2));
+                    wt[k * MROWS + r] = st.x;
+                    const float next = fmaxf(top, st.x);
+                    if (next > -INFINITY) sum = sum * ex2(top - next) + st.y * ex2(st.x - next);
+                    top = next;
+                }
+                const float inv = 1.f / sum;
+                for (int k = 0; k < n; ++k) wt[k * MROWS + r] = top == -INFINITY ? inv : ex2(wt[k * MROWS + r] - top) * inv;
+            }
+            bar_softmax();
+            const int RP = rows > 64 ? 128 : rows > 32 ? 64 : 32, groups = min(128 / RP, HD / 32), row = tid & (RP - 1), cols = HD / groups;
+            if (row < rows && tid / RP < groups) {
+                const long long to_row = row_offset(p, x.b, h, r0 + row, HD);
+#pragma unroll 1
+                for (int c = (tid / RP) * cols; c < (tid / RP + 1) * cols; c += 32) {
+                    float4 acc[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                    for (int k = 0; k < n; ++k) {
+                        const float4 *src = reinterpret_cast<const float4 *>(piece(k)) + (size_t)c / 4 * w.rows + row;
+                        float4 y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + (size_t)j * w.rows);
+                        const float al = wt[k * MROWS + row];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            acc[j].x = fmaf(y[j].x, al, acc[j].x); acc[j].y = fmaf(y[j].y, al, acc[j].y);
+                            acc[j].z = fmaf(y[j].z, al, acc[j].z); acc[j].w = fmaf(y[j].w, al, acc[j].w);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2)
+                        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + to_row + c + j * 4) =
+                            make_uint4(pack_bf16(acc[j].x, acc[j].y), pack_bf16(acc[j].z, acc[j].w), pack_bf16(acc[j + 1].x, acc[j + 1].y),
+                                       pack_bf16(acc[j + 1].z, acc[j + 1].w));
+                }
+            }
+            bar_softmax();                         // (the weights' place is the next query rows')
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == MMA) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TM_COLS));
+    }
+    if (tid == 0 && *abort_flag && p.status) atomicOr(p.status, ORTHRUS_DEV_WAIT_TIMEOUT);
+}
+
+// [rows][d], boxes of `box` rows and 64 columns
+bool page_map(const void *ptr, unsigned d, unsigned long long rows, unsigned box, CUtensorMap *out)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)d * 2};
+    const cuuint32_t boxes[2] = {64, box}, estr[2] = {1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD>
+cudaError_t launch_one(const PagedParams &p, const PagedMaps &tm, const PagedWork &w, int ctas, cudaStream_t st)
+{
+    using C = Shape<HD>;
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = configure(paged_attend_tc_kernel<HD>, done, C::SMEM, false);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(p.early, paged_attend_tc_kernel<HD>, dim3(ctas), NTHREADS, C::SMEM, st, p, tm, w);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_attend_wide(const PagedParams &p, const PagedWork &w, unsigned long long rows, int ctas, cudaStream_t st)
+{
+    PagedMaps tm;
+    if (!page_map(p.k_pages, p.d, rows, 1u << w.box_shift, &tm.k) || !page_map(p.v_pages, p.d, rows, 1u << w.box_shift, &tm.v))
+        return cudaErrorInvalidValue;
+    return p.d == 128 ? launch_one<128>(p, tm, w, ctas, st) : launch_one<64>(p, tm, w, ctas, st);
+}
+
+}  // namespace orthrus
