@@ -62,7 +62,7 @@ orthrus_status_t attend(const orthrus_paged_layer_t *L, int causal, const void *
     p.early = !(L->flags & ORTHRUS_LAYER_NO_EARLY_LAUNCH);
     p.quiescent = (L->flags & ORTHRUS_LAYER_CACHE_QUIESCENT) != 0;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    if (!tc) set_last_path("simt");
+    set_last_path(tc ? "tcgen05" : "simt");
     const cudaError_t e = tc ? launch_paged_attend_tc(p, *L, static_cast<unsigned char *>(ws) + kHeaderBytes, cs)
                              : launch_paged_attend_simt(p, L->dtype, cs);
     return e == cudaSuccess ? ORTHRUS_OK : ORTHRUS_ERR_CUDA;

@@ -1,19 +1,31 @@
-// Attention over the pages of a paged cache for units of more than 16 query rows, bf16, head_dim 64 and 128, on tcgen05: blocks of either
-// view, wide groups.  Work is cut and pieces are joined as in paged_attend_mma.cu (which see); a unit's query tile is 128 rows.
+// Attention over the pages of a paged cache, bf16, head_dim 64 and 128, on tcgen05: one new token a request, blocks of either view.
 //
-//   S [128 rows x 64 keys] = Q K^T          O [128 rows x d] += P V,  P = 2^(S scale - reference)
+//   S [128 rows x 64 keys] = Q K^T          O [128 rows x d] += P V,  P = 2^(S scale - reference)          (S scale in the log2 domain)
 //
-// What bounds it: HBM up to some 64 rows, then the softmax (64 exponentials a row and tile) and the MMAs.  Rows that a unit does not have
-// are padding of the MMA, but cost no softmax.  CTA of 192 threads, 113 KB of shared memory and 256 TMEM columns: two fit an SM, so that one's
-// softmax overlaps the other's products.
+// One pass over the keys with a running reference and sum; a unit is a request, a KV head and up to 128 of its query rows (G heads by K
+// block positions).  Rows that a unit does not have are padding of the MMA, but cost no softmax.
+//
+// What bounds it: HBM, 4 d bytes per key and KV head, up to some 64 rows; then the softmax (64 exponentials a row and tile) and the MMAs.  For a
+// decoding step of 4 to 16 rows warp-level MMAs of 16 rows were built first and taken out: they spend more instructions on a tile than
+// one thread here that issues it (32 requests of 1024 to 8192 keys, 4 rows: 109 us against 94).
+//
+// Work is cut by tiles of 64 keys, not by requests: all tiles of all units lie on one line, and CTA c of n takes the stretch
+// [c T / n, (c + 1) T / n).  Every CTA finds its stretch from the lengths themselves, so that the host needs no plan, a captured graph serves any
+// lengths, and a batch of unequal requests loads all SMs alike.  A unit that is cut leaves pieces (unnormalised sums with their
+// reference) in the workspace; the CTA that finishes last, by the unit's counter, joins them in the order of their keys, which fixes the result.
+//
+// CTA of 192 threads, 113 KB of shared memory and 256 TMEM columns: two fit an SM, so that one's softmax overlaps the other's products, and the
+// next call's CTAs can be resident early.
 //   warps 0-3  softmax, thread = query row: scores from tensor memory, probabilities back to it as bf16 in their place; also the
 //              query rows' way into shared memory, the read-out, and the join
-//   warp 4     producer: K and V tiles into a ring of slots, a TMA box per page and 64 columns
+//   warp 4     producer: looks up pages, K and V tiles into a ring of slots, a TMA box per page and 64 columns, running on into the
+//              next unit of the stretch
 //   warp 5     MMAs: the scores of the next tile are issued ahead of the product of this one
 // A row's reference follows its maximum only when that has grown by more than 2^8 since: the output in tensor memory is rescaled rarely,
 // numerator and denominator use the same reference, and probabilities stay below 2^8.
 // Every wait is bounded: on expiry the CTA raises ORTHRUS_DEV_WAIT_TIMEOUT, waits for its copies and MMAs in flight and ends.
 #include <cuda.h>
+#include <type_traits>
 #include "paged_stretch.cuh"
 
 namespace orthrus {
@@ -34,14 +46,15 @@ template <int HD> struct Shape {
     static constexpr int PANELS = HD / 64, QSUB = MROWS * 128, SUB = KT * 128, SLOT = PANELS * SUB;   // bytes
     static constexpr int NSLOT = HD == 128 ? 5 : 10;
     static constexpr int OFF_Q = 0, OFF_RING = PANELS * QSUB, OFF_BAR = OFF_RING + NSLOT * SLOT;
-    // barriers: slots full, slots empty, scores (two buffers), probabilities (two), products done, query rows, drained
+    // barriers: slots full, slots empty, scores (two buffers), probabilities (two), a product done, query rows, all products of a
+    // unit done (a waiter at the unit's end may find the barrier of the single ones two phases behind), drained
     static constexpr int FULL = 0, EMPTY = NSLOT, SCORES = 2 * NSLOT, PROBS = SCORES + 2, PRODUCT = PROBS + 2, QUERY = PRODUCT + 1,
-                         DRAIN = QUERY + 1, BARS = DRAIN + 1;
+                         DONE = QUERY + 1, DRAIN = DONE + 1, BARS = DRAIN + 1;
     static constexpr int OFF_MISC = OFF_BAR + BARS * 8, SMEM = OFF_MISC + 16;
     static constexpr uint32_t TM_S = HD, TM_COLS = 256;            // O, then two buffers of scores
-    // the join: weights of the pieces [piece][row], in the place of the query rows
-    static constexpr int MOST = PANELS * QSUB / (MROWS * 4);
-    static_assert(2 * (SMEM + 1024) <= 228 * 1024 && kMostWide <= MOST, "two CTAs per SM; the join");
+    // the join: references and sums of the pieces [piece][row], in the place of the query rows
+    static constexpr int JOIN = PANELS * QSUB;
+    static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
 };
 
 template <int HD>
@@ -167,6 +180,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                     for (int kk = 0; kk < KT / 16; ++kk) umma_ts(tmem, a + kk * 8, vd + (kk * 2048 >> 4), IDESC_PV, t > 0 || kk > 0);
                     umma_commit(bar(C::EMPTY + slot));
                     umma_commit(bar(C::PRODUCT));
+                    if (t == tiles - 1) umma_commit(bar(C::DONE));
                 }
                 __syncwarp();
             }
@@ -184,7 +198,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
         const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
         bool ok = find_stretch(p, U, blockIdx.x, gridDim.x, w.most_pieces, lane, false, s);
         const long long start = ok ? s.pos : 0;
-        int T = 0;
+        int T = 0, units = 0;
         while (ok && next_piece(p, s, start, lane, x)) {
             const int h = x.u / w.row_tiles, r0 = (x.u - h * w.row_tiles) * MROWS, M = x.n * p.G, keys = x.P + x.n;
             const int rows = max(0, min(MROWS, M - r0));
@@ -273,7 +287,8 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::PROBS + (T & 1)));
             }
-            if (ok) ok = mbar_wait_warp(bar(C::PRODUCT), (T - 1) & 1, abort_flag);
+            if (ok) ok = mbar_wait_warp(bar(C::DONE), units & 1, abort_flag);
+            ++units;
             ok = bar_softmax_and(ok);              // (a warp whose wait ran out has come here too: all leave together)
             if (!ok) break;
             tc_fence_after();
@@ -325,52 +340,77 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
             }
             bar_softmax();
             if (!*last_flag || rows == 0) continue;
-            // The join.  Weights first (a thread its row), in the place of the query rows; then `groups` threads share a row's columns.
-            const float *first = w.pieces + (2 * c0 + (s.T * c0 / s.n == x.unit0 ? 0 : 1)) * step, *others = w.pieces + 2 * c0 * step;
+            // The join, in the place of the query rows: the pieces' references and sums, from them their weights, by a thread a row; then
+            // every thread sums up vectors of four columns, in the order in which they lie in the pieces.
+            const float *first = w.pieces + (2 * c0 + (quotient(s.T * c0, s.n) == x.unit0 ? 0 : 1)) * step, *others = w.pieces + 2 * c0 * step;
             auto piece = [&](int k) { return k ? others + 2 * k * step : first; };
-            float *wt = reinterpret_cast<float *>(smem + C::OFF_Q);
-            if (r < rows) {
-                float top = -INFINITY, sum = 0.f;
-#pragma unroll 8
-                for (int k = 0; k < n; ++k) {
-                    const float2 st = __ldcg(reinterpret_cast<const float2 *>(piece(k) + stats + r * 2));
-                    wt[k * MROWS + r] = st.x;
-                    const float next = fmaxf(top, st.x);
-                    if (next > -INFINITY) sum = sum * ex2(top - next) + st.y * ex2(st.x - next);
-                    top = next;
-                }
-                const float inv = 1.f / sum;
-                for (int k = 0; k < n; ++k) wt[k * MROWS + r] = top == -INFINITY ? inv : ex2(wt[k * MROWS + r] - top) * inv;
+            float2 *wt = reinterpret_cast<float2 *>(smem + C::OFF_Q);                  // [piece][row]
+            for (int e = tid; e < n * rows; e += 128) {
+                const int k = e / rows;
+                wt[e] = __ldcg(reinterpret_cast<const float2 *>(piece(k) + stats) + (e - k * rows));
             }
             bar_softmax();
-            const int RP = rows > 64 ? 128 : rows > 32 ? 64 : 32, groups = min(128 / RP, HD / 32), row = tid & (RP - 1), cols = HD / groups;
-            if (row < rows && tid / RP < groups) {
-                const long long to_row = row_offset(p, x.b, h, r0 + row, HD);
+            if (r < rows) {
+                float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+                for (int k = 0; k < n; ++k) top = fmaxf(top, wt[k * rows + r].x);
+                const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+                for (int k = 0; k < n; ++k) {
+                    const float2 st = wt[k * rows + r];
+                    const float al = ex2(st.x - from);
+                    sum = fmaf(st.y, al, sum);
+                    wt[k * rows + r].x = al;
+                }
+                wt[r].y = 1.f / sum;
+            }
+            bar_softmax();
+            // IT vectors of UN pieces under way together
+            auto sum_up = [&](auto it, auto un) {
+                constexpr int IT = decltype(it)::value, UN = decltype(un)::value;
+                const int vecs = rows * (HD / 4);
 #pragma unroll 1
-                for (int c = (tid / RP) * cols; c < (tid / RP + 1) * cols; c += 32) {
-                    float4 acc[8];
+                for (int e0 = tid; e0 < vecs; e0 += 128 * IT) {
+                    float4 acc[IT];
+                    int row[IT], off[IT];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-                    for (int k = 0; k < n; ++k) {
-                        const float4 *src = reinterpret_cast<const float4 *>(piece(k)) + (size_t)c / 4 * w.rows + row;
-                        float4 y[8];
+                    for (int i = 0; i < IT; ++i) {
+                        const int e = min(e0 + i * 128, vecs - 1), c = e / rows;      // (past the end the last one again, not stored)
+                        acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        row[i] = e - c * rows;
+                        off[i] = c * w.rows + row[i];
+                    }
+#pragma unroll 1
+                    for (int k0 = 0; k0 < n; k0 += UN) {
+                        float4 y[UN][IT];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) y[j] = __ldcg(src + (size_t)j * w.rows);
-                        const float al = wt[k * MROWS + row];
+                        for (int u = 0; u < UN; ++u) {
+                            const float4 *src = reinterpret_cast<const float4 *>(piece(min(k0 + u, n - 1)));      // (likewise)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            acc[j].x = fmaf(y[j].x, al, acc[j].x); acc[j].y = fmaf(y[j].y, al, acc[j].y);
-                            acc[j].z = fmaf(y[j].z, al, acc[j].z); acc[j].w = fmaf(y[j].w, al, acc[j].w);
+                            for (int i = 0; i < IT; ++i) y[u][i] = __ldcg(src + off[i]);
                         }
+#pragma unroll
+                        for (int u = 0; u < UN; ++u)
+                            if (k0 + u < n)
+#pragma unroll
+                                for (int i = 0; i < IT; ++i) {
+                                    const float al = wt[(k0 + u) * rows + row[i]].x;
+                                    acc[i].x = fmaf(y[u][i].x, al, acc[i].x); acc[i].y = fmaf(y[u][i].y, al, acc[i].y);
+                                    acc[i].z = fmaf(y[u][i].z, al, acc[i].z); acc[i].w = fmaf(y[u][i].w, al, acc[i].w);
+                                }
                     }
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2)
-                        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + to_row + c + j * 4) =
-                            make_uint4(pack_bf16(acc[j].x, acc[j].y), pack_bf16(acc[j].z, acc[j].w), pack_bf16(acc[j + 1].x, acc[j + 1].y),
-                                       pack_bf16(acc[j + 1].z, acc[j + 1].w));
+                    for (int i = 0; i < IT; ++i) {
+                        const int e = e0 + i * 128;
+                        if (e >= vecs) break;
+                        const float inv = wt[row[i]].y;
+                        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + row_offset(p, x.b, h, r0 + row[i], HD) + e / rows * 4) =
+                            make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
+                    }
                 }
-            }
+            };
+            if (rows * (HD / 4) <= 128) sum_up(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
+            else sum_up(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
             bar_softmax();                         // (the weights' place is the next query rows')
         }
     }
@@ -406,12 +446,53 @@ cudaError_t launch_one(const PagedParams &p, const PagedMaps &tm, const PagedWor
 
 }  // namespace
 
-cudaError_t launch_paged_attend_wide(const PagedParams &p, const PagedWork &w, unsigned long long rows, int ctas, cudaStream_t st)
+bool paged_tc_shape(const orthrus_paged_layer_t &L)
 {
+    if (L.dtype != ORTHRUS_BF16 || (L.head_dim != 64 && L.head_dim != 128) || L.page_size < 16) return false;
+    return (unsigned long long)L.n_pages * L.n_kv_heads * L.page_size < 0x7fffffffull && tc_driver_ok();
+}
+
+// CTAs of a call, and what its workspace holds: from the shape and the host's bound on the lengths.
+namespace {
+struct Grid { int ctas, row_tiles, rows, most_pieces; size_t counters, bytes; };
+Grid plan(const orthrus_paged_layer_t &L)
+{
+    Grid g;
+    const int M = L.n_q_heads / L.n_kv_heads * L.block;
+    g.row_tiles = (M + MROWS - 1) / MROWS;
+    g.rows = M < MROWS ? M : MROWS;
+    const long long units = (long long)L.batch * L.n_kv_heads * g.row_tiles;
+    const long long keys = (L.max_len_hint > 0 ? (long long)L.max_len_hint : (long long)L.max_pages * L.page_size - L.block) + L.block;
+    const long long tiles = units * (((keys < 1 ? 1 : keys) + KT - 1) / KT);
+    // Two CTAs an SM where there is much to stream; one where latency counts, which halves the pieces to join
+    const long long most = (tiles >= 16LL * num_sms() ? 2LL : 1LL) * num_sms();
+    g.ctas = (int)(tiles < 1 ? 1 : tiles < most ? tiles : most);
+    // pieces of a unit: what the join has room for, and no more than one CTA adds up in the time the others save
+    const int room = (L.head_dim == 128 ? Shape<128>::JOIN : Shape<64>::JOIN) / (g.rows * 8);
+    g.most_pieces = room < 32 ? room : 32;
+    g.counters = (size_t)((units * 4 + 255) / 256 * 256);
+    g.bytes = g.counters + 2 * (size_t)g.ctas * piece_floats(g.rows, L.head_dim) * sizeof(float);
+    return g;
+}
+}  // namespace
+
+size_t paged_tc_workspace_bytes(const orthrus_paged_layer_t &L) { return plan(L).bytes; }
+
+cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_layer_t &L, void *ws_body, cudaStream_t st)
+{
+    const Grid g = plan(L);
+    PagedWork w;
+    w.row_tiles = g.row_tiles;
+    w.box_shift = p.page_shift < 6 ? p.page_shift : 6;
+    w.rows = g.rows;
+    w.most_pieces = g.most_pieces;
+    w.counter = static_cast<int *>(ws_body);
+    w.pieces = reinterpret_cast<float *>(static_cast<unsigned char *>(ws_body) + g.counters);
     PagedMaps tm;
+    const unsigned long long rows = (unsigned long long)L.n_pages * L.n_kv_heads * L.page_size;
     if (!page_map(p.k_pages, p.d, rows, 1u << w.box_shift, &tm.k) || !page_map(p.v_pages, p.d, rows, 1u << w.box_shift, &tm.v))
         return cudaErrorInvalidValue;
-    return p.d == 128 ? launch_one<128>(p, tm, w, ctas, st) : launch_one<64>(p, tm, w, ctas, st);
+    return p.d == 128 ? launch_one<128>(p, tm, w, g.ctas, st) : launch_one<64>(p, tm, w, g.ctas, st);
 }
 
 }  // namespace orthrus

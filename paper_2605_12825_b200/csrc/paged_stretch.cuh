@@ -1,5 +1,4 @@
-// What the two tensor-core kernels of the paged attention share: how a batch's work is cut over CTAs, pieces of units and their join's
-// bookkeeping, the tensor maps of a pool of pages.
+// How the work of a paged attention call is cut over CTAs, where the pieces of its units lie, and the walk over a request's pages.
 #pragma once
 #include <cuda.h>
 #include "paged.cuh"
@@ -10,8 +9,6 @@ namespace orthrus {
 constexpr int KT = 64;                    // keys per tile
 constexpr int kLeast = 2;                 // tiles a CTA takes at least, while there are fewer than CTAs
 
-constexpr int kMostNarrow = 48, kMostWide = 24;      // pieces of a unit at most, in units of up to 16 query rows and of more
-
 struct PagedMaps { CUtensorMap k, v; };
 struct PagedWork {
     int row_tiles;           // tiles of query rows of a (request, KV head)
@@ -19,11 +16,16 @@ struct PagedWork {
     int rows;                // query rows a piece holds: min(rows of a tile, K G)
     int most_pieces;         // pieces of a unit
     int *counter;            // [unit]: pieces that are in
-    float *pieces;           // [2 CTAs] pieces: an output of rows x d, behind it [rows][2] (maximum, sum)
+    float *pieces;           // [2 CTAs] pieces: an output [d / 4][rows][4], behind it [rows][2] (reference, sum)
 };
 
 // floats of a piece, a multiple of the 16 bytes it is moved in
 __host__ __device__ constexpr size_t piece_floats(int rows, int d) { return ((size_t)rows * (d + 2) + 3) / 4 * 4; }
+
+// (of numbers that hardly ever pass 32 bits)
+__device__ inline long long quotient(long long a, long long b) {
+    return (unsigned long long)(a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
 
 // A CTA's stretch of the line of tiles, piece by piece.  Every warp walks it by itself, 32 requests' lengths in its lanes.
 struct Stretch {
@@ -76,11 +78,11 @@ __device__ inline bool find_stretch(const PagedParams &p, int U, int c, int ctas
     s.T = sum * U;
     if (s.T == 0) return false;
     long long n = min((long long)ctas, (s.T + kLeast - 1) / kLeast);
-    n = min(n, max(1ll, s.T * (most - 1) / longest));
+    n = min(n, max(1ll, quotient(s.T * (most - 1), longest)));
     s.n = (int)n;
     if (c >= s.n) return false;
-    s.pos = s.T * c / n;
-    s.end = s.T * (c + 1) / n;
+    s.pos = quotient(s.T * c, n);
+    s.end = quotient(s.T * (c + 1), n);
     // the request that the stretch begins in
     long long run = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32) {
@@ -107,7 +109,7 @@ __device__ inline bool next_piece(const PagedParams &p, Stretch &s, long long st
         set_request(p, s, lane);
     }
     x.b = s.b; x.P = s.P; x.n = s.rows; x.tiles = s.tiles;
-    x.u = (int)((s.pos - s.base) / s.tiles);
+    x.u = (int)quotient(s.pos - s.base, s.tiles);
     x.unit0 = s.base + (long long)x.u * s.tiles;
     x.t0 = (int)(s.pos - x.unit0);
     x.t1 = (int)min((long long)s.tiles, x.t0 + (s.end - s.pos));
@@ -115,7 +117,7 @@ __device__ inline bool next_piece(const PagedParams &p, Stretch &s, long long st
     s.pos += x.t1 - x.t0;
     return true;
 }
-__device__ inline int owner(const Stretch &s, long long tile) { return (int)(((tile + 1) * s.n - 1) / s.T); }
+__device__ inline int owner(const Stretch &s, long long tile) { return (int)quotient((tile + 1) * s.n - 1, s.T); }
 
 // Rows of q and out: row R of request b and KV head h
 __device__ inline long long row_offset(const PagedParams &p, int b, int h, int R, int d)
@@ -148,8 +150,5 @@ struct PageWindow {
         return pg;
     }
 };
-
-// host side
-struct PagedGrid { int ctas, row_tiles, rows, most_pieces; size_t counters, bytes; };
 
 }  // namespace orthrus
