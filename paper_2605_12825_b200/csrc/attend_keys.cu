@@ -60,7 +60,7 @@
 #include <float.h>
 #include <atomic>
 #include <mutex>
-#include "common.cuh"
+#include "paged.cuh"
 #include "tc_ptx.cuh"
 
 namespace orthrus {
@@ -85,6 +85,14 @@ struct KeysArgs {
     int tiles;                 // query tiles of a unit; blockIdx.y = tile * KV heads + head
 };
 
+// PAGED: the cache is a pool of pages; the block's keys are in it, behind the prefix, and no keys of their own
+struct KeysPages {
+    const int32_t *table, *n_new;          // [B][max_pages]; [B] rows of the block that exist, or null
+    int page_shift, max_pages, max_pos, box_shift;     // box: rows of a TMA box, min(page, 64)
+    int n_pages;
+};
+constexpr int kPagesHeld = 64;             // table entries of a CTA that are kept in shared memory
+
 template <int HD, int NR> struct KeysShape {
     static constexpr int PANELS = HD / 64;
     static constexpr int KV_BYTES = PANELS * PANEL;
@@ -108,7 +116,7 @@ template <int HD, int NR> struct KeysShape {
                          BAR_QKALL = BAR_PV + 2, BAR_ALL = BAR_QKALL + 1, BAR_DRAIN = BAR_ALL + 1,
                          BAR_X = BAR_DRAIN + 1, NUM_BARS = BAR_X + 1;
     static constexpr int OFF_MISC = OFF_BAR + NUM_BARS * 8;    // TMEM address, abort flag, sequence
-    static constexpr int SMEM_BYTES = OFF_MISC + 16;
+    static constexpr int OFF_PAGES = OFF_MISC + 16, SMEM_BYTES = OFF_PAGES, SMEM_PAGED = OFF_PAGES + kPagesHeld * 4;
     // the merge, in the ring: [task of this CTA][CTA] messages, then weights [warp][CTA][row]
     static constexpr int TASKS = NR / 4 * (HD / 32);
     static constexpr int OFF_XW = (TASKS + MAX_CLUSTER) * MSG;
@@ -117,7 +125,7 @@ template <int HD, int NR> struct KeysShape {
     static constexpr uint32_t TM_COLS = 4 * NR;                // two score buffers, two accumulators
     static constexpr uint32_t tm_s(int w) { return (uint32_t)(w * NR); }
     static constexpr uint32_t tm_o(int w) { return (uint32_t)(2 * NR + w * NR); }
-    static_assert(CTAS * (SMEM_BYTES + 1024) <= 228 * 1024, "shared memory of an SM");
+    static_assert(CTAS * (SMEM_PAGED + 1024) <= 228 * 1024, "shared memory of an SM");
 };
 
 __device__ inline float warp_max(float x) {
@@ -232,9 +240,12 @@ __device__ inline BlockPart block_part(const __nv_bfloat16 *q, const __nv_bfloat
 // they wait for messages (8 units of 64 rows, 4096 keys and blocks of 16: sixteen CTAs of two tiles each).
 // The code is kept short on purpose (loops not unrolled, one place for each wait, copy and product): the warps' roles are
 // run through once or twice per call, and an SM's instruction cache holds 32 KB.
-template <int HD, int NR, bool XCH, bool APART>
-__device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps &tm, const KeysArgs &args)
+// PAGED: the keys are rows of pages, found through the request's table.  The halves run over prefix and block alike; of the block's rows,
+// which a call brings M of, only those exist that n_new says.
+template <int HD, int NR, bool XCH, bool APART, bool PAGED = false>
+__device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps &tm, const KeysArgs &args, const KeysPages &pg)
 {
+    static_assert(!(APART && PAGED), "a block in pages is a part of the tiles");
     using C = KeysShape<HD, NR>;
     constexpr int PANELS = C::PANELS, QPANEL = NR * 128;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -258,7 +269,9 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
     // ------------------------------------------------------------------ prologue
     int b = blockIdx.z, P = 0;
     const bool len_first = quiescent && !args.ranked;         // the length is on its way while the barriers are set up
+    int rows = p.K;                                            // of the block, that exist
     if (len_first) P = p.cache_len[b];
+    if (PAGED && len_first && pg.n_new) rows = pg.n_new[b];
     // The producer is to ask for its first tiles as early as can be: it sets up the barriers of the ring and waits for nobody.
     if (warp == PRODUCER_WARP) {
         if (lane == 0) {
@@ -277,7 +290,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             fence_proxy_async();
             if (XCH) mbar_expect_tx(bar(C::BAR_X), (uint32_t)(my_tasks * S * MSG));
-            if (!APART) { prefetch_map(&tm.kb); prefetch_map(&tm.vb); }
+            if (!APART && !PAGED) { prefetch_map(&tm.kb); prefetch_map(&tm.vb); }
         }
         __syncwarp();
         bar_issue_arrive();
@@ -290,7 +303,10 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
     // which unit: when the clusters do not all fit at once they go out longest prefix first (every warp finds out by itself)
     if (__builtin_expect(!quiescent, 0)) griddep_wait();
     const int h = blockIdx.y - zt * p.Hkv;
-    const int len_hi = (int)p.len_cap;
+    if (PAGED && !len_first && pg.n_new) rows = pg.n_new[b];
+    const int rows_hi = PAGED ? min(p.K, pg.max_pos) : 0, rows_given = rows;
+    if (PAGED) rows = min(max(rows, 0), rows_hi);
+    const int len_hi = PAGED ? pg.max_pos - rows : (int)p.len_cap;
     if (__builtin_expect(args.ranked, 0)) b = rank_by_length(p, b, len_hi, lane);
     if (!len_first) P = p.cache_len[b];
     if (warp != PRODUCER_WARP) {
@@ -298,19 +314,25 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
         bar_start_wait();
         tc_fence_after();
     }
-    if (P < 0 || P > len_hi) {
+    if (P < 0 || P > len_hi || (PAGED && rows_given != rows)) {
         if (tid == 0 && rank == 0 && p.status) atomicOr(p.status, ORTHRUS_DEV_BAD_CACHE_LEN);
-        P = P < 0 ? 0 : len_hi;
+        P = PAGED ? min(max(P, 0), len_hi) : P < 0 ? 0 : len_hi;
     }
     // the unit's halves: n_pre of 64 prefix keys, then the block's keys, shared out evenly
-    const int n_pre = (P + HALF - 1) / HALF, n_all = n_pre + !APART;
+    const int keys = P + rows;                                // PAGED: of the request; the halves below are of all of them, n_pre of
+                                                              // them the prefix's alone
+    const int n_pre = PAGED ? P / HALF : (P + HALF - 1) / HALF;
+    const int n_all = PAGED ? (rows > 0 ? (keys + HALF - 1) / HALF : 0) : n_pre + !APART;
     const int share = XCH ? (int)__umulhi((unsigned)n_all, args.inv_s32) : n_all, rest = n_all - share * S;
     auto first_half = [&](int k) { return XCH ? k * share + (int)((uint32_t)(k * rest) * args.inv_s >> 16) : k * share; };  // k * n_all / S
     const int a0 = first_half(rank), a1 = first_half(rank + 1);
     const int nh = a1 - a0, n_mine = max(0, min(nh, n_pre - a0));     // halves of this CTA, prefix halves among them
     const int n_tiles = (nh + 1) >> 1;
     // keys of half a (CTA-local): 0 past the end
-    auto half_keys = [&](int a) { return a >= nh ? 0 : (a < n_mine ? min(HALF, P - (a0 + a) * HALF) : p.K); };
+    auto half_keys = [&](int a) {
+        if (PAGED) return a >= nh ? 0 : min(HALF, keys - (a0 + a) * HALF);
+        return a >= nh ? 0 : (a < n_mine ? min(HALF, P - (a0 + a) * HALF) : p.K);
+    };
 
     // ring items in the order of their use: K0, K1, V0, K2, V1, ..., K(n-1), V(n-2), V(n-1); item i in slot i % NSLOT, or,
     // folded, K0, K1, V0 in slots 0 to 2 and V1 in slot 1
@@ -321,7 +343,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
     auto item_of_k = [&](int t) { return t == 0 ? 0 : 2 * t - 1; };
     auto item_of_v = [&](int t) { return min(2 * t + 2, 2 * n_tiles - 1); };
     const int n_slots = C::NSLOT + fold;
-    const int row_base = (int)(((long long)(b / p.nb) * p.Hkv + h) * p.capacity);
+    const int row_base = PAGED ? 0 : (int)(((long long)(b / p.nb) * p.Hkv + h) * p.capacity);
     // half a (CTA-local) of a K or V tile, to its place in `slot`
     const uint64_t policy = policy_evict_first();
     auto load_half = [&](bool v, int a, int slot) {
@@ -335,6 +357,30 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
         }
     };
     constexpr int HALF_BYTES = PANELS * HALF * 128;
+    // PAGED: halves [a, last) of an item (one or two), a lane a box of page rows and 64 columns; who calls it is a whole warp
+    auto load_pages = [&](bool v, int a, int last, int slot) {
+        const int boxes = HALF >> pg.box_shift, per_half = boxes * PANELS;
+        const int half = a + lane / per_half, i = lane % per_half % boxes, pan = lane % per_half / boxes;      // (at most 16 lanes)
+        const int pos = (a0 + half) * HALF + (i << pg.box_shift);
+        uint32_t bytes = 0;
+#pragma unroll 1
+        for (int x = a; x < last; ++x) bytes += (uint32_t)((half_keys(x) + (1 << pg.box_shift) - 1) >> pg.box_shift) * PANELS * (128u << pg.box_shift);
+        const uint32_t fb = bar(C::BAR_FULL + slot);
+        if (lane == 0) mbar_expect_tx(fb, bytes);
+        __syncwarp();
+        if (lane < 2 * per_half && half < last && pos < keys) {
+            const int j = pos >> pg.page_shift, k = j - (a0 * HALF >> pg.page_shift);
+            int page = k < kPagesHeld ? reinterpret_cast<const int *>(smem + C::OFF_PAGES)[k] : __ldg(pg.table + (long long)b * pg.max_pages + j);
+            if (page < 0 || page >= pg.n_pages) {
+                if (p.status) atomicOr(p.status, ORTHRUS_DEV_BAD_PAGE);
+                page = 0;
+            }
+            const int row = ((page * p.Hkv + h) << pg.page_shift) + (pos & ((1 << pg.page_shift) - 1));
+            tma_load_2d(sbase + C::OFF_RING + slot * C::KV_BYTES + pan * PANEL + (half & 1) * (HALF * 128) + (i << pg.box_shift) * 128, v ? &tm.v : &tm.k,
+                        pan * 64, row, fb, policy);
+        }
+        __syncwarp();
+    };
 
     if (warp < SW) {
         // ------------------------------------------------------------------ query rows
@@ -354,7 +400,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
 #pragma unroll
             for (int u = 0; u < QN; ++u) {
                 const int e = tid + u * ST, r = e / QCH;
-                q_src[u] = r < M ? row_off(r) / 8 + e % QCH : -1;
+                q_src[u] = r < (PAGED ? min(M, (rows - i0) * p.G) : M) ? row_off(r) / 8 + e % QCH : -1;
                 // (a line that the preceding kernel is writing may be asked into L2: that is where it is written)
                 if (q_src[u] >= 0 && (lane & 7) == 0) prefetch_l2(q + q_src[u]);
             }
@@ -390,7 +436,9 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
         for (int t = wg, u = 0; t < n_tiles; t += 2, ++u) {
             const int a = 2 * t + (kt >> 6), j = kt & 63;     // this thread's half and key in it
             // rows below lo do not see the key (all, if the key does not exist)
-            const int lo = j >= half_keys(a) ? NR : (!APART && a >= n_mine && p.causal ? (j - i0) * p.G : 0);
+            const int lo = j >= half_keys(a) ? NR
+                           : PAGED ? (p.causal ? ((a0 + a) * HALF + j - P - i0) * p.G : 0)
+                           : (!APART && a >= n_mine && p.causal ? (j - i0) * p.G : 0);
             const bool masks = __any_sync(0xffffffffu, lo > 0);
             if (u > 0) mbar_wait_warp_call(bar(C::BAR_PV + wg), (u - 1) & 1, abort_flag);   // P buffer and O^T at rest
             mbar_wait_warp_call(bar(C::BAR_S + wg), u & 1, abort_flag);
@@ -594,7 +642,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
                 } else {
 #pragma unroll
                     for (int i = 0; i < CR; ++i)
-                        if (c + i < M) out[row_off(c + i) + d] = __float2bfloat16_rn(x[i]);
+                        if (c + i < (PAGED ? min(M, (rows - i0) * p.G) : M)) out[row_off(c + i) + d] = __float2bfloat16_rn(x[i]);
                 }
             }
         }
@@ -607,7 +655,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
             auto places = [&](int n) {
                 const int task = n * S + rank, g = task / (HD / 32), col = task % (HD / 32) * 32 + lane;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) at[k] = 4 * g + k < M ? row_off(4 * g + k) + col : -1;
+                for (int k = 0; k < 4; ++k) at[k] = 4 * g + k < (PAGED ? min(M, (rows - i0) * p.G) : M) ? row_off(4 * g + k) + col : -1;
             };
             float *wt = reinterpret_cast<float *>(smem + C::OFF_XW) + warp * ((MAX_CLUSTER + 1) * 4);
             bool got = true;
@@ -687,7 +735,52 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
     } else if (warp == PRODUCER_WARP) {
         // ------------------------------------------------------------------ producer
         bar_issue_wait();                                     // the other barriers are set up
-        if (lane == 0) {
+        if constexpr (PAGED) {
+            // this CTA's table entries, then as below, a whole warp
+            const int *first = pg.table + (long long)b * pg.max_pages + (a0 * HALF >> pg.page_shift);
+            const int n_held = min(kPagesHeld, nh > 0 ? ((min(a1 * HALF, keys) - 1) >> pg.page_shift) - (a0 * HALF >> pg.page_shift) + 1 : 0);
+            for (int k = lane; k < n_held; k += 32) reinterpret_cast<int *>(smem + C::OFF_PAGES)[k] = __ldg(first + k);
+            __syncwarp();
+            const int n_items = 2 * n_tiles;
+            bool ok = (sbase & 1023u) == 0;
+            uint32_t loaded = 0;
+            int n = 0;
+#pragma unroll 1
+            for (bool ahead = quiescent; ; ++n) {
+                if (ahead && (n >= n_items || n >= n_slots)) {
+                    griddep_wait();
+                    ahead = false; n = 0;
+                }
+                if (!ahead && (n >= n_items || !ok)) break;
+                const bool v = n == n_items - 1 || (n > 0 && (n & 1) == 0);
+                const int t = v ? (n == n_items - 1 ? n_tiles - 1 : n / 2 - 1) : (n + 1) / 2;
+                const int slot = slot_of(n), last = min(2 * t + 2, nh);
+                if (ahead) {
+                    if (last > n_mine) continue;              // (rows of the block are among them)
+                } else {
+                    if (n < 32 && (loaded >> n & 1)) continue;
+                    if (use_of(n) > 0) {
+                        // (as below)
+                        const int i = fold ? 1 : n - C::NSLOT;
+                        const bool iv = i > 0 && (i & 1) == 0;
+                        const int it = iv ? i / 2 - 1 : C::NSLOT == 4 && i == 0 ? 1 : (i + 1) / 2;
+                        ok = mbar_wait_warp_call(bar((iv ? C::BAR_PV : C::BAR_S) + (it & 1)), (it >> 1) & 1, abort_flag);
+                        if (!ok) continue;
+                    }
+                }
+                if (n < 32) loaded |= 1u << n;
+                load_pages(v, 2 * t, last, slot);
+            }
+            if (lane == 0 && __builtin_expect(*abort_flag, 0)) {
+                const int end = ok ? n : max(n - 1, 0);
+#pragma unroll 1
+                for (int i = fold ? 0 : max(0, end - C::NSLOT); i < max(end, n_slots); ++i) {
+                    int dummy = 0;
+                    if (fold && i == 1 && (loaded >> 3 & 1)) continue;
+                    if (i < 32 ? loaded >> i & 1 : i < end) mbar_wait_call(bar(C::BAR_FULL + slot_of(i)), use_of(i) & 1, &dummy);
+                }
+            }
+        } else if (lane == 0) {
             const int n_items = 2 * n_tiles;
             bool ok = (sbase & 1023u) == 0;
             // Two rounds.  The first only if the caller promised that the preceding kernel writes no cache row below
@@ -756,7 +849,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
         constexpr uint32_t IDESC_PV = keys_idesc(NR, 1, 1);   // A = V tile, B = P, both MN-major
         const uint32_t tmem = *tmem_slot;
         bool ok = __all_sync(0xffffffffu, !*abort_flag);
-        if (!APART && quiescent && nh > n_mine) {
+        if (!APART && !PAGED && quiescent && nh > n_mine) {
             // the block's own half of the last tile, where the producer's first round has left it out
             griddep_wait();
             if (ok && elect_one()) {
@@ -811,7 +904,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
 #pragma unroll 1
                     for (int a = 0; a < 2; ++a) {
                         const int n = a ? k1 : k0, pad = -n & 15;
-                        if (pad && (2 * pt + a < n_mine || p.blk_in_cache)) {
+                        if (pad && (PAGED || 2 * pt + a < n_mine || p.blk_in_cache)) {
                             unsigned char *vt = smem + C::OFF_RING + slot * C::KV_BYTES + a * (HALF * 128);
 #pragma unroll 1
                             for (int e = lane; e < pad * (HD / 8); e += 32)
@@ -860,13 +953,19 @@ template <int HD, int NR, bool XCH>
 __global__ void __launch_bounds__(NTHREADS, KeysShape<HD, NR>::CTAS)
 attend_keys_kernel(const AttnParams p, const __grid_constant__ KeysMaps tm, const KeysArgs args)
 {
-    attend_keys<HD, NR, XCH, false>(p, tm, args);
+    attend_keys<HD, NR, XCH, false>(p, tm, args, KeysPages());
 }
 template <int HD, int NR>
 __global__ void __launch_bounds__(NTHREADS, KeysShape<HD, NR>::CTAS)
 apart_attend_keys_kernel(const AttnParams p, const __grid_constant__ KeysMaps tm, const KeysArgs args)
 {
-    attend_keys<HD, NR, true, true>(p, tm, args);
+    attend_keys<HD, NR, true, true>(p, tm, args, KeysPages());
+}
+template <int HD, int NR, bool XCH>
+__global__ void __launch_bounds__(NTHREADS, KeysShape<HD, NR>::CTAS)
+paged_attend_keys_kernel(const AttnParams p, const __grid_constant__ KeysMaps tm, const KeysArgs args, const __grid_constant__ KeysPages pg)
+{
+    attend_keys<HD, NR, XCH, false, true>(p, tm, args, pg);
 }
 template <int HD, int NR, bool XCH, bool APART> constexpr auto keys_kernel()
 {
@@ -993,6 +1092,30 @@ cudaError_t launch_shape(const AttnParams &p, const KeysMaps &tm, int flags, cud
     return e;
 }
 
+// over pages
+template <int HD, int NR, bool XCH = true>
+cudaError_t launch_paged_shape(const AttnParams &p, const KeysMaps &tm, const KeysPages &pg, int quiescent, cudaStream_t st)
+{
+    if constexpr (XCH)
+        if (p.n_splits == 1) return launch_paged_shape<HD, NR, false>(p, tm, pg, quiescent, st);
+    using C = KeysShape<HD, NR>;
+    static std::atomic<uint64_t> done{0};
+    auto kern = paged_attend_keys_kernel<HD, NR, XCH>;
+    const cudaError_t e = configure(kern, done, C::SMEM_PAGED, true);
+    if (e != cudaSuccess) return e;
+    const int S = p.n_splits, kb = keys_kb_rows(HD, p.G, p.K), tiles = (p.K + kb - 1) / kb;
+    KeysArgs args;
+    args.S = S;
+    args.quiescent = quiescent;
+    args.ranked = 0;
+    args.inv_g = (65536u + p.G - 1) / p.G;
+    args.inv_s = (65536u + S - 1) / S;
+    args.inv_s32 = (uint32_t)(((1ull << 32) + S - 1) / S);
+    args.kb_rows = kb;
+    args.tiles = tiles;
+    return launch_clusters(p.early, S, kern, dim3(S, p.Hkv * tiles, p.B), NTHREADS, C::SMEM_PAGED, st, p, tm, args, pg);
+}
+
 template <int HD>
 cudaError_t launch_rows(const AttnParams &p, const KeysMaps &tm, int flags, cudaStream_t st)
 {
@@ -1070,6 +1193,47 @@ cudaError_t launch_attend_keys(const AttnParams &p, int flags, cudaStream_t st)
         return cudaErrorInvalidValue;
     }
     return p.d == 64 ? launch_rows<64>(p, tm, flags, st) : launch_rows<128>(p, tm, flags, st);
+}
+
+// CTAs of a cluster for a call over pages (0: not a shape of this kernel, or its clusters are not all resident)
+int paged_keys_splits(const orthrus_paged_layer_t &L, int max_len)
+{
+    const int G = L.n_q_heads / L.n_kv_heads, d = L.head_dim, nr = keys_rows(d, G, L.block);
+    if (!nr || L.batch > 65535) return 0;
+    const int kb = keys_kb_rows(d, G, L.block), tiles = (L.block + kb - 1) / kb;
+    const long long units = (long long)L.batch * L.n_kv_heads * tiles;
+    const int per_sm = nr <= 64 ? 2 : 1;
+    if ((long long)L.n_kv_heads * tiles > 65535 || units > 2 * num_sms()) return 0;
+    bool apart = false;
+    const long long all = (long long)max_len + L.block - HALF;          // (as keys_splits counts: the block a half of its own)
+    const int S = keys_splits(d, G, L.block, (int)units, all < 0 ? 0 : (int)all, &apart);
+    return units <= clusters_resident(S, per_sm) ? S : 0;
+}
+
+cudaError_t launch_paged_attend_keys(const PagedParams &pp, int S, cudaStream_t st)
+{
+    AttnParams p = {};
+    p.q = pp.q; p.cache_len = pp.cache_len; p.out = pp.out; p.status = pp.status;
+    p.B = pp.B; p.K = pp.K; p.Hq = pp.Hq; p.Hkv = pp.Hkv; p.G = pp.G; p.M = pp.G * pp.K; p.d = pp.d;
+    p.n_splits = S; p.causal = pp.causal; p.blk_in_cache = 1; p.nb = 1; p.scale_log2 = pp.scale_log2; p.early = pp.early;
+    KeysPages pg;
+    pg.table = pp.table; pg.n_new = pp.n_new; pg.page_shift = pp.page_shift; pg.max_pages = pp.max_pages; pg.max_pos = pp.max_pos;
+    pg.box_shift = pp.page_shift < 6 ? pp.page_shift : 6; pg.n_pages = (int)pp.n_pages;
+    KeysMaps tm;
+    const unsigned long long rows = (unsigned long long)pp.n_pages * pp.Hkv << pp.page_shift;
+    if (!page_map(pp.k_pages, p.d, rows, 1u << pg.box_shift, &tm.k) || !page_map(pp.v_pages, p.d, rows, 1u << pg.box_shift, &tm.v))
+        return cudaErrorInvalidValue;
+    tm.kb = tm.k; tm.vb = tm.v;                   // (not used)
+    const int nr = keys_rows(p.d, p.G, p.K);
+    if (p.d == 128)
+        return nr == 16 ? launch_paged_shape<128, 16>(p, tm, pg, pp.quiescent, st)
+             : nr == 32 ? launch_paged_shape<128, 32>(p, tm, pg, pp.quiescent, st) : launch_paged_shape<128, 64>(p, tm, pg, pp.quiescent, st);
+    switch (nr) {
+    case 16: return launch_paged_shape<64, 16>(p, tm, pg, pp.quiescent, st);
+    case 32: return launch_paged_shape<64, 32>(p, tm, pg, pp.quiescent, st);
+    case 64: return launch_paged_shape<64, 64>(p, tm, pg, pp.quiescent, st);
+    }
+    return launch_paged_shape<64, 128>(p, tm, pg, pp.quiescent, st);
 }
 
 }  // namespace orthrus

@@ -1,5 +1,6 @@
 // Declarations of the paged-cache calls: what their translation units share.
 #pragma once
+#include <cuda.h>
 #include <atomic>
 #include "common.cuh"
 
@@ -40,6 +41,11 @@ cudaError_t launch_paged_attend_simt(const PagedParams &p, int dtype, cudaStream
 bool paged_tc_shape(const orthrus_paged_layer_t &L);        // the tensor-core kernel serves this shape
 size_t paged_tc_workspace_bytes(const orthrus_paged_layer_t &L);
 cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_layer_t &L, void *ws_body, cudaStream_t st);
+
+int paged_keys_splits(const orthrus_paged_layer_t &L, int max_len);       // attend_keys.cu: few query rows, where latency counts
+cudaError_t launch_paged_attend_keys(const PagedParams &p, int S, cudaStream_t st);
+// a pool as [rows][d], boxes of `box` rows and 64 columns, 128-byte swizzle
+bool page_map(const void *ptr, unsigned d, unsigned long long rows, unsigned box, CUtensorMap *out);
 
 // prefix length and rows of request b, clamped to what the layer can hold (`bad`: they had to be)
 __device__ inline void paged_request(const PagedParams &p, int b, int &P, int &n, bool &bad)

@@ -26,6 +26,7 @@
 // Every wait is bounded: on expiry the CTA raises ORTHRUS_DEV_WAIT_TIMEOUT, waits for its copies and MMAs in flight and ends.
 #include <cuda.h>
 #include <type_traits>
+#include <cstdlib>
 #include "paged_stretch.cuh"
 
 namespace orthrus {
@@ -423,17 +424,6 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
     if (tid == 0 && *abort_flag && p.status) atomicOr(p.status, ORTHRUS_DEV_WAIT_TIMEOUT);
 }
 
-// [rows][d], boxes of `box` rows and 64 columns
-bool page_map(const void *ptr, unsigned d, unsigned long long rows, unsigned box, CUtensorMap *out)
-{
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[2] = {d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)d * 2};
-    const cuuint32_t boxes[2] = {64, box}, estr[2] = {1, 1};
-    return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int HD>
 cudaError_t launch_one(const PagedParams &p, const PagedMaps &tm, const PagedWork &w, int ctas, cudaStream_t st)
 {
@@ -445,6 +435,16 @@ cudaError_t launch_one(const PagedParams &p, const PagedMaps &tm, const PagedWor
 }
 
 }  // namespace
+
+bool page_map(const void *ptr, unsigned d, unsigned long long rows, unsigned box, CUtensorMap *out)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)d * 2};
+    const cuuint32_t boxes[2] = {64, box}, estr[2] = {1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 bool paged_tc_shape(const orthrus_paged_layer_t &L)
 {
@@ -480,6 +480,10 @@ size_t paged_tc_workspace_bytes(const orthrus_paged_layer_t &L) { return plan(L)
 
 cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_layer_t &L, void *ws_body, cudaStream_t st)
 {
+    const int max_len = L.max_len_hint > 0 ? L.max_len_hint : p.max_pos > p.K ? p.max_pos - p.K : 0;
+    const int S = paged_keys_splits(L, max_len);
+    const char *pk = getenv("PK");
+    if (S > 0 && pk && pk[0] == '1') return launch_paged_attend_keys(p, S, st);
     const Grid g = plan(L);
     PagedWork w;
     w.row_tiles = g.row_tiles;
