@@ -71,6 +71,7 @@ static Knobs read_knobs()
     return k;
 }
 bool early_launch_allowed() { return !read_knobs().no_early_launch; }
+int small_rows_knob() { return read_knobs().small_rows; }
 
 }  // namespace orthrus
 

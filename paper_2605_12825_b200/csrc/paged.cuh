@@ -35,6 +35,7 @@ struct PagedParams {
     float scale_log2;
     int early, quiescent;   // launch as a programmatic dependent; first tiles ahead of the preceding kernel
 };
+int small_rows_knob();                      // ORTHRUS_TC_SMALL_ROWS: 0, 1, or -1 where it is not set
 bool simt_forced();                         // orthrus_set_path("simt")
 void set_last_path(const char *name);       // what orthrus_last_path() answers on this thread; a literal
 cudaError_t launch_paged_attend_simt(const PagedParams &p, int dtype, cudaStream_t st);
@@ -47,11 +48,12 @@ cudaError_t launch_paged_attend_keys(const PagedParams &p, int S, cudaStream_t s
 // a pool as [rows][d], boxes of `box` rows and 64 columns, 128-byte swizzle
 bool page_map(const void *ptr, unsigned d, unsigned long long rows, unsigned box, CUtensorMap *out);
 
-// prefix length and rows of request b, clamped to what the layer can hold (`bad`: they had to be)
+// Prefix length and rows of request b, clamped to what the layer can hold (`bad`: they had to be).  Read past L1, where a look ahead of
+// the wait for the preceding kernel could have left what that kernel then changed.
 __device__ inline void paged_request(const PagedParams &p, int b, int &P, int &n, bool &bad)
 {
-    P = p.cache_len[b];
-    n = p.n_new ? p.n_new[b] : p.K;
+    P = __ldcg(p.cache_len + b);
+    n = p.n_new ? __ldcg(p.n_new + b) : p.K;
     bad = n < 0 || n > p.K;
     n = min(max(n, 0), min(p.K, p.max_pos));
     bad |= P < 0 || P > p.max_pos - n;

@@ -26,7 +26,6 @@
 // Every wait is bounded: on expiry the CTA raises ORTHRUS_DEV_WAIT_TIMEOUT, waits for its copies and MMAs in flight and ends.
 #include <cuda.h>
 #include <type_traits>
-#include <cstdlib>
 #include "paged_stretch.cuh"
 
 namespace orthrus {
@@ -43,9 +42,10 @@ __device__ inline bool bar_softmax_and(bool ok) {
     return r != 0;
 }
 
-template <int HD> struct Shape {
-    static constexpr int PANELS = HD / 64, QSUB = MROWS * 128, SUB = KT * 128, SLOT = PANELS * SUB;   // bytes
-    static constexpr int NSLOT = HD == 128 ? 5 : 10;
+// QR: query rows that have a place.  Of a product's 128 rows those behind them are whatever lies there, and nobody reads their results.
+template <int HD, int QR> struct Shape {
+    static constexpr int PANELS = HD / 64, QSUB = QR * 128, SUB = KT * 128, SLOT = PANELS * SUB;   // bytes
+    static constexpr int NSLOT = (113 * 1024 - PANELS * QSUB - 512) / SLOT;
     static constexpr int OFF_Q = 0, OFF_RING = PANELS * QSUB, OFF_BAR = OFF_RING + NSLOT * SLOT;
     // barriers: slots full, slots empty, scores (two buffers), probabilities (two), a product done, query rows, all products of a
     // unit done (a waiter at the unit's end may find the barrier of the single ones two phases behind), drained
@@ -55,14 +55,14 @@ template <int HD> struct Shape {
     static constexpr uint32_t TM_S = HD, TM_COLS = 256;            // O, then two buffers of scores
     // the join: references and sums of the pieces [piece][row], in the place of the query rows
     static constexpr int JOIN = PANELS * QSUB;
-    static_assert(2 * (SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
+    static_assert(NSLOT >= 5 && 2 * (SMEM + 1024) <= 228 * 1024 && OFF_RING + NSLOT * SLOT >= MROWS * 128 + (PANELS - 1) * QSUB, "two CTAs per SM");
 };
 
-template <int HD>
+template <int HD, int QR>
 __global__ void __launch_bounds__(NTHREADS, 2)
 paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedMaps tm, const __grid_constant__ PagedWork w)
 {
-    using C = Shape<HD>;
+    using C = Shape<HD, QR>;
     constexpr int NSLOT = C::NSLOT, PANELS = C::PANELS;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t sbase = smem_u32(smem);
@@ -96,41 +96,49 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
         // ------------------------------------------------------------------ producer
         bool waited = false;
         auto wait = [&] { griddep_wait(); griddep_launch(); waited = true; };
-        if (!p.quiescent) wait();
         int items = 0;
         if (lane == 0) { prefetch_map(&tm.k); prefetch_map(&tm.v); }
-        if (find_stretch(p, U, blockIdx.x, gridDim.x, w.most_pieces, lane, blockIdx.x == 0, s)) {
-            const long long start = s.pos;
-            const uint64_t policy = policy_evict_first();
-            const int box = 1 << w.box_shift;
-            bool ok = true;
-            PageWindow pages;
-            while (ok && next_piece(p, s, start, lane, x)) {
-                const int h = x.u / w.row_tiles, keys = x.P + x.n;
-                pages.open(p, x, lane);
-                for (int t = x.t0; ok && t < x.t1; ++t) {
-                    const int pos0 = t * KT;
-                    if (!waited && pos0 + KT > x.P) wait();                                   // rows of the block itself
-                    const int last = min(pos0 + KT, keys) - 1;
-                    const int i = lane & 3, pan = lane >> 2;                                  // lane: box and panel
-                    const int pos = pos0 + (i << w.box_shift), pg = pages.page(p, pos, last, lane);
-                    const int live = ((last - pos0) >> w.box_shift) + 1;
-                    const int row = ((pg * p.Hkv + h) << p.page_shift) + (pos & (page - 1));
+        // The stretch is looked for ahead of the wait.  Unless the lengths are promised, it is a guess, which is made again behind the wait if they
+        // have changed; the pages are looked up behind it.
+        PageWindow pages;
+        bool have;
+#pragma unroll 1
+        for (bool again = false; ; again = true) {
+            s = find_stretch(p, U, w.most_pieces);
+            have = next_piece(p, s, lane, x);
+            if (!p.quiescent && !again) wait();
+            if (have) pages.open(p, x, lane);
+            if (p.quiescent || again || still_so(p, s, lane)) break;
+        }
+        const uint64_t policy = policy_evict_first();
+        const int box = 1 << w.box_shift;
+        bool ok = true;
+        while (ok && have) {
+            const int h = x.u / w.row_tiles, keys = x.P + x.n;
+            for (int t = x.t0; ok && t < x.t1; ++t) {
+                const int pos0 = t * KT;
+                if (!waited && pos0 + KT > x.P) wait();                                   // rows of the block itself
+                const int last = min(pos0 + KT, keys) - 1;
+                const int i = lane & 3, pan = lane >> 2;                                  // lane: box and panel
+                const int pos = pos0 + (i << w.box_shift), pg = pages.page(p, pos, last, lane);
+                const int live = ((last - pos0) >> w.box_shift) + 1;
+                const int row = ((pg * p.Hkv + h) << p.page_shift) + (pos & (page - 1));
 #pragma unroll
-                    for (int kind = 0; kind < 2; ++kind) {
-                        const int slot = items % NSLOT;
-                        if (items >= NSLOT) ok = mbar_wait_warp(bar(C::EMPTY + slot), (items / NSLOT + 1) & 1, abort_flag);
-                        if (!ok) break;
-                        if (lane == 0) mbar_expect_tx(bar(C::FULL + slot), live * box * HD * 2);
-                        __syncwarp();
-                        if (lane < 4 * PANELS && i < live)
-                            tma_load_2d(sbase + C::OFF_RING + slot * C::SLOT + pan * C::SUB + i * (box * 128), kind ? &tm.v : &tm.k, pan * 64, row,
-                                        bar(C::FULL + slot), policy);
-                        __syncwarp();
-                        ++items;
-                    }
+                for (int kind = 0; kind < 2; ++kind) {
+                    const int slot = items % NSLOT;
+                    if (items >= NSLOT) ok = mbar_wait_warp_call(bar(C::EMPTY + slot), (items / NSLOT + 1) & 1, abort_flag);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(bar(C::FULL + slot), live * box * HD * 2);
+                    __syncwarp();
+                    if (lane < 4 * PANELS && i < live)
+                        tma_load_2d(sbase + C::OFF_RING + slot * C::SLOT + pan * C::SUB + i * (box * 128), kind ? &tm.v : &tm.k, pan * 64, row,
+                                    bar(C::FULL + slot), policy);
+                    __syncwarp();
+                    ++items;
                 }
             }
+            have = ok && next_piece(p, s, lane, x);
+            if (have) pages.open(p, x, lane);
         }
         if (!waited) wait();
         if (*abort_flag && lane == 0)                   // the last copies, before the block can end
@@ -138,13 +146,18 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
         __syncwarp();
     } else if (warp == MMA) {
         // ------------------------------------------------------------------ MMAs
-        griddep_wait();
         constexpr uint32_t IDESC_QK = make_idesc(KT, 0), IDESC_PV = make_idesc(HD, 1);
         const uint64_t q_desc = make_desc(sbase + C::OFF_Q, 16, 1024);
-        bool ok = find_stretch(p, U, blockIdx.x, gridDim.x, w.most_pieces, lane, false, s);
-        const long long start = ok ? s.pos : 0;
+        bool ok = true;
+#pragma unroll 1
+        for (bool again = false; ; again = true) {
+            s = find_stretch(p, U, w.most_pieces);
+            if (!again) griddep_wait();
+            if (again || still_so(p, s, lane)) break;
+        }
+        if (blockIdx.x == 0) tell_requests(p, lane);
         int T = 0, units = 0;
-        auto full = [&](int item) { return mbar_wait_warp(bar(C::FULL + item % NSLOT), (item / NSLOT) & 1, abort_flag); };
+        auto full = [&](int item) { return mbar_wait_warp_call(bar(C::FULL + item % NSLOT), (item / NSLOT) & 1, abort_flag); };
         auto scores = [&](int T) {
             const int slot = 2 * T % NSLOT;
             if (elect_one()) {
@@ -158,9 +171,9 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
             }
             __syncwarp();
         };
-        while (ok && next_piece(p, s, start, lane, x)) {
+        while (ok && next_piece(p, s, lane, x)) {
             const int tiles = x.t1 - x.t0;
-            ok = mbar_wait_warp(bar(C::QUERY), units & 1, abort_flag) && full(2 * T);
+            ok = mbar_wait_warp_call(bar(C::QUERY), units & 1, abort_flag) && full(2 * T);
             if (!ok) break;
             tc_fence_after();
             scores(T);
@@ -170,7 +183,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                     if (!ok) break;
                     scores(T + 1);
                 }
-                ok = mbar_wait_warp(bar(C::PROBS + (T & 1)), (T >> 1) & 1, abort_flag) && full(2 * T + 1);
+                ok = mbar_wait_warp_call(bar(C::PROBS + (T & 1)), (T >> 1) & 1, abort_flag) && full(2 * T + 1);
                 if (!ok) break;
                 tc_fence_after();
                 const int slot = (2 * T + 1) % NSLOT;
@@ -194,27 +207,35 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
         }
     } else {
         // ------------------------------------------------------------------ softmax
-        griddep_wait();
         const int r = tid;
         const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
-        bool ok = find_stretch(p, U, blockIdx.x, gridDim.x, w.most_pieces, lane, false, s);
-        const long long start = ok ? s.pos : 0;
-        int T = 0, units = 0;
-        while (ok && next_piece(p, s, start, lane, x)) {
-            const int h = x.u / w.row_tiles, r0 = (x.u - h * w.row_tiles) * MROWS, M = x.n * p.G, keys = x.P + x.n;
-            const int rows = max(0, min(MROWS, M - r0));
-            const bool at_work = warp * 32 < rows;       // (other warps have padding only)
-            const long long at = r < rows ? row_offset(p, x.b, h, r0 + r, HD) : 0;
-            // this thread's query row, into swizzled panels of 64 columns; a row that does not exist is left as it is
-            if (r < rows) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + at);
-                uint4 v[HD / 8];
-#pragma unroll
-                for (int c = 0; c < HD / 8; ++c) v[c] = src[c];
+        int T = 0, units = 0, h, r0, keys, rows;
+        long long at;
+        auto open = [&] {                                // the unit, and this thread's query row
+            const int M = x.n * p.G;
+            h = x.u / w.row_tiles, r0 = (x.u - h * w.row_tiles) * MROWS, keys = x.P + x.n;
+            rows = max(0, min(MROWS, M - r0));
+            at = r < rows ? row_offset(p, x.b, h, r0 + r, HD) : 0;
+            // into swizzled panels of 64 columns; a row that does not exist is left as it is
+            const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(p.q) + at;
+            const uint32_t dst = sbase + C::OFF_Q + r * 128;
+            if (r < rows)
 #pragma unroll
                 for (int c = 0; c < HD / 8; ++c)
-                    *reinterpret_cast<uint4 *>(smem + C::OFF_Q + (c >> 3) * C::QSUB + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[c];
-            }
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (c >> 3) * C::QSUB + (((c & 7) ^ (r & 7)) << 4)), "l"(src + c * 8) : "memory");
+        };
+        bool have = false, ok = true;
+#pragma unroll 1
+        for (int look = 0; ; ++look) {                   // first and second look at the lengths, then unit after unit
+            if (look < 2) s = find_stretch(p, U, w.most_pieces);
+            have = next_piece(p, s, lane, x);
+            if (look == 0) griddep_wait();
+            if (have) open();
+            if (look == 0 && !still_so(p, s, lane)) { asm volatile("cp.async.wait_all;" ::: "memory"); continue; }
+            if (look == 0) look = 1;
+            if (!have) break;
+            const bool at_work = warp * 32 < rows;       // (other warps have padding only)
+            asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::QUERY));
@@ -223,7 +244,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
             for (int t = x.t0; t < x.t1; ++t, ++T) {
                 const int pos0 = t * KT;
                 const uint32_t ts = mine + C::TM_S + (T & 1) * KT;
-                if (!mbar_wait_warp(bar(C::SCORES + (T & 1)), (T >> 1) & 1, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp_call(bar(C::SCORES + (T & 1)), (T >> 1) & 1, abort_flag)) { ok = false; break; }
                 tc_fence_after();
                 if (at_work) {
                     uint32_t raw[KT];
@@ -247,7 +268,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                         l *= al;
                         if (t > x.t0) {
                             // the products so far, which are the sums up to the tile before
-                            if (!mbar_wait_warp(bar(C::PRODUCT), (T - 1) & 1, abort_flag)) { ok = false; break; }
+                            if (!mbar_wait_warp_call(bar(C::PRODUCT), (T - 1) & 1, abort_flag)) { ok = false; break; }
                             tc_fence_after();
 #pragma unroll 1
                             for (int c = 0; c < HD; c += 32) {
@@ -276,7 +297,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 if (pos0 + KT > keys) {
                     // rows behind the last key, which may hold anything: zero, for the product with their zero probabilities
                     const int item = 2 * T + 1, slot = item % NSLOT;
-                    if (!mbar_wait_warp(bar(C::FULL + slot), (item / NSLOT) & 1, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait_warp_call(bar(C::FULL + slot), (item / NSLOT) & 1, abort_flag)) { ok = false; break; }
                     const int n0 = keys - pos0, n = (KT - n0) * (HD / 8);
                     for (int e = tid; e < n; e += 128) {
                         const int row = n0 + e / (HD / 8), c = e % (HD / 8);
@@ -288,131 +309,128 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::PROBS + (T & 1)));
             }
-            if (ok) ok = mbar_wait_warp(bar(C::DONE), units & 1, abort_flag);
+            if (ok) ok = mbar_wait_warp_call(bar(C::DONE), units & 1, abort_flag);
             ++units;
             ok = bar_softmax_and(ok);              // (a warp whose wait ran out has come here too: all leave together)
             if (!ok) break;
             tc_fence_after();
-            if (x.t0 == 0 && x.t1 == x.tiles) {
-                if (at_work) {
-                    const float inv = 1.f / l;
+            // this thread's row of the output, 64 columns at a time
+            auto read_out = [&](auto put) {
 #pragma unroll 1
-                    for (int c = 0; c < HD; c += 32) {
-                        uint32_t raw[32];
-                        float o[32];
-                        tmem_ld32(mine + c, raw);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(raw[j]);
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8)
-                            st_global_if(r < rows, static_cast<__nv_bfloat16 *>(p.out) + at + c + j,
-                                         make_uint4(pack_bf16(o[j] * inv, o[j + 1] * inv), pack_bf16(o[j + 2] * inv, o[j + 3] * inv),
-                                                    pack_bf16(o[j + 4] * inv, o[j + 5] * inv), pack_bf16(o[j + 6] * inv, o[j + 7] * inv)));
-                    }
-                    tc_fence_before();
-                }
-                continue;
-            }
-            // a piece: [four columns][row], so that a warp's store is 512 contiguous bytes
-            const size_t step = piece_floats(w.rows, HD), stats = (size_t)w.rows * HD;
-            float *to = w.pieces + (2 * blockIdx.x + (x.first ? 0 : 1)) * step;
-            if (at_work) {
-#pragma unroll 1
-                for (int c = 0; c < HD; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(mine + c, o);
+                for (int c = 0; c < HD; c += 64) {
+                    uint32_t o[64];
+                    tmem_ld<64>(mine + c, o);
                     tmem_ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4)
-                        st_global_if(r < rows, to + ((size_t)(c + j) / 4 * w.rows + r) * 4, make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+                    put(c, o);
                 }
                 tc_fence_before();
-                if (r < rows) *reinterpret_cast<float2 *>(to + stats + r * 2) = make_float2(ref, l);
-            }
-            const int c0 = owner(s, x.unit0), n = owner(s, x.unit0 + x.tiles - 1) - c0 + 1;
-            bar_softmax();
-            if (tid == 0) {
-                int *counter = w.counter + (long long)x.b * U + x.u;
-                __threadfence();
-                const bool last = atomicAdd(counter, 1) == n - 1;
-                if (last) { *counter = 0; __threadfence(); }
-                *last_flag = last;
-            }
-            bar_softmax();
-            if (!*last_flag || rows == 0) continue;
-            // The join, in the place of the query rows: the pieces' references and sums, from them their weights, by a thread a row; then
-            // every thread sums up vectors of four columns, in the order in which they lie in the pieces.
-            const float *first = w.pieces + (2 * c0 + (quotient(s.T * c0, s.n) == x.unit0 ? 0 : 1)) * step, *others = w.pieces + 2 * c0 * step;
-            auto piece = [&](int k) { return k ? others + 2 * k * step : first; };
-            float2 *wt = reinterpret_cast<float2 *>(smem + C::OFF_Q);                  // [piece][row]
-            for (int e = tid; e < n * rows; e += 128) {
-                const int k = e / rows;
-                wt[e] = __ldcg(reinterpret_cast<const float2 *>(piece(k) + stats) + (e - k * rows));
-            }
-            bar_softmax();
-            if (r < rows) {
-                float top = -INFINITY, sum = 0.f;
-#pragma unroll 4
-                for (int k = 0; k < n; ++k) top = fmaxf(top, wt[k * rows + r].x);
-                const float from = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
-                for (int k = 0; k < n; ++k) {
-                    const float2 st = wt[k * rows + r];
-                    const float al = ex2(st.x - from);
-                    sum = fmaf(st.y, al, sum);
-                    wt[k * rows + r].x = al;
-                }
-                wt[r].y = 1.f / sum;
-            }
-            bar_softmax();
-            // IT vectors of UN pieces under way together
-            auto sum_up = [&](auto it, auto un) {
-                constexpr int IT = decltype(it)::value, UN = decltype(un)::value;
-                const int vecs = rows * (HD / 4);
-#pragma unroll 1
-                for (int e0 = tid; e0 < vecs; e0 += 128 * IT) {
-                    float4 acc[IT];
-                    int row[IT], off[IT];
-#pragma unroll
-                    for (int i = 0; i < IT; ++i) {
-                        const int e = min(e0 + i * 128, vecs - 1), c = e / rows;      // (past the end the last one again, not stored)
-                        acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        row[i] = e - c * rows;
-                        off[i] = c * w.rows + row[i];
-                    }
-#pragma unroll 1
-                    for (int k0 = 0; k0 < n; k0 += UN) {
-                        float4 y[UN][IT];
-#pragma unroll
-                        for (int u = 0; u < UN; ++u) {
-                            const float4 *src = reinterpret_cast<const float4 *>(piece(min(k0 + u, n - 1)));      // (likewise)
-#pragma unroll
-                            for (int i = 0; i < IT; ++i) y[u][i] = __ldcg(src + off[i]);
-                        }
-#pragma unroll
-                        for (int u = 0; u < UN; ++u)
-                            if (k0 + u < n)
-#pragma unroll
-                                for (int i = 0; i < IT; ++i) {
-                                    const float al = wt[(k0 + u) * rows + row[i]].x;
-                                    acc[i].x = fmaf(y[u][i].x, al, acc[i].x); acc[i].y = fmaf(y[u][i].y, al, acc[i].y);
-                                    acc[i].z = fmaf(y[u][i].z, al, acc[i].z); acc[i].w = fmaf(y[u][i].w, al, acc[i].w);
-                                }
-                    }
-#pragma unroll
-                    for (int i = 0; i < IT; ++i) {
-                        const int e = e0 + i * 128;
-                        if (e >= vecs) break;
-                        const float inv = wt[row[i]].y;
-                        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + row_offset(p, x.b, h, r0 + row[i], HD) + e / rows * 4) =
-                            make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
-                    }
-                }
             };
-            if (rows * (HD / 4) <= 128) sum_up(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
-            else sum_up(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
-            bar_softmax();                         // (the weights' place is the next query rows')
+            const bool uncut = x.t0 == 0 && x.t1 == x.tiles;
+            if (uncut && at_work) {
+                const float inv = 1.f / l;
+                read_out([&](int c, const uint32_t (&o)[64]) {
+#pragma unroll
+                    for (int j = 0; j < 64; j += 8) {
+                        auto two = [&](int i) { return pack_bf16(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv); };
+                        st_global_if(r < rows, static_cast<__nv_bfloat16 *>(p.out) + at + c + j, make_uint4(two(j), two(j + 2), two(j + 4), two(j + 6)));
+                    }
+                });
+            }
+            if (!uncut) {
+                // a piece: [four columns][row], so that a warp's store is 512 contiguous bytes
+                const size_t step = piece_floats(w.rows, HD), stats = (size_t)w.rows * HD;
+                if (at_work) {
+                    float *to = w.pieces + (2 * blockIdx.x + (x.first ? 0 : 1)) * step;
+                    if (r < rows) *reinterpret_cast<float2 *>(to + stats + r * 2) = make_float2(ref, l);
+                    read_out([&](int c, const uint32_t (&o)[64]) {
+#pragma unroll
+                        for (int j = 0; j < 64; j += 4)
+                            st_global_if(r < rows, to + ((size_t)(c + j) / 4 * w.rows + r) * 4, make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+                    });
+                }
+                const int c0 = owner(s, x.unit0), n = owner(s, x.unit0 + x.tiles - 1) - c0 + 1;
+                bar_softmax();
+                if (tid == 0) {
+                    // (releases what the barrier's other threads have stored, acquires what the other CTAs have)
+                    int *counter = w.counter + (long long)x.b * U + x.u, before;
+                    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+                    if (before == n - 1) *counter = 0;
+                    *last_flag = before == n - 1;
+                }
+                // The join of the CTA that is the last.  Where things lie does not depend on it; vectors of four columns, a row a lane of them
+                const int rs = rows > 1 ? 32 - __clz(rows - 1) : 0;                      // log2 of the rows, rounded up
+                const int vecs = HD / 4 << rs;
+                const float *others = w.pieces + 2 * c0 * step, *first = others + (stretch_start(s, c0) == x.unit0 ? 0 : step);
+                auto piece = [&](int k) { return k ? others + 2 * k * step : first; };
+                bar_softmax();
+                if (*last_flag && rows > 0) {
+                    float2 *st = reinterpret_cast<float2 *>(smem + C::OFF_Q);            // [piece][row]: references and sums, in the query rows' place
+                    for (int e = tid; e < n << rs; e += 128) {
+                        const int k = e >> rs, row = e & ((1 << rs) - 1);
+                        if (row < rows) st[e] = __ldcg(reinterpret_cast<const float2 *>(piece(k) + stats) + row);
+                    }
+                    // IT vectors of UN pieces under way together
+                    auto sum_up = [&](auto it, auto un) {
+                        constexpr int IT = decltype(it)::value, UN = decltype(un)::value;
+#pragma unroll 1
+                        for (int e0 = tid; e0 - tid < vecs; e0 += 128 * IT) {
+                            float4 acc[IT];
+                            float top[IT], sum[IT];
+                            int row[IT], off[IT];
+#pragma unroll
+                            for (int i = 0; i < IT; ++i) {
+                                const int e = e0 + i * 128;
+                                row[i] = min(e & ((1 << rs) - 1), rows - 1);             // (rows and vectors that do not exist: another, not stored)
+                                off[i] = min(e >> rs, HD / 4 - 1) * w.rows + row[i];
+                                acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                top[i] = -INFINITY;
+                                sum[i] = 0.f;
+                            }
+#pragma unroll 1
+                            for (int k0 = 0; k0 < n; k0 += UN) {
+                                float4 y[UN][IT];
+#pragma unroll
+                                for (int u = 0; u < UN; ++u) {
+                                    const float4 *src = reinterpret_cast<const float4 *>(piece(min(k0 + u, n - 1)));      // (likewise)
+#pragma unroll
+                                    for (int i = 0; i < IT; ++i) y[u][i] = __ldcg(src + off[i]);
+                                }
+                                if (k0 == 0) {
+                                    if (e0 == tid) bar_softmax();                        // (the references are there)
+#pragma unroll 4
+                                    for (int k = 0; k < n; ++k)
+#pragma unroll
+                                        for (int i = 0; i < IT; ++i) top[i] = fmaxf(top[i], st[(k << rs) + row[i]].x);
+#pragma unroll
+                                    for (int i = 0; i < IT; ++i) if (top[i] == -INFINITY) top[i] = 0.f;
+                                }
+#pragma unroll
+                                for (int u = 0; u < UN; ++u)
+                                    if (k0 + u < n)
+#pragma unroll
+                                        for (int i = 0; i < IT; ++i) {
+                                            const float2 rf = st[((k0 + u) << rs) + row[i]];
+                                            const float al = ex2(rf.x - top[i]);
+                                            sum[i] = fmaf(rf.y, al, sum[i]);
+                                            acc[i].x = fmaf(y[u][i].x, al, acc[i].x); acc[i].y = fmaf(y[u][i].y, al, acc[i].y);
+                                            acc[i].z = fmaf(y[u][i].z, al, acc[i].z); acc[i].w = fmaf(y[u][i].w, al, acc[i].w);
+                                        }
+                            }
+#pragma unroll
+                            for (int i = 0; i < IT; ++i) {
+                                const int e = e0 + i * 128;
+                                if (e >= vecs || (e & ((1 << rs) - 1)) >= rows) continue;
+                                const float inv = 1.f / sum[i];
+                                *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + row_offset(p, x.b, h, r0 + row[i], HD) + (e >> rs) * 4) =
+                                    make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
+                            }
+                        }
+                    };
+                    if (vecs <= 256) sum_up(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
+                    else sum_up(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+                    bar_softmax();                         // (the references' place is the next query rows')
+                }
+            }
         }
     }
     tc_fence_before();
@@ -424,14 +442,14 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
     if (tid == 0 && *abort_flag && p.status) atomicOr(p.status, ORTHRUS_DEV_WAIT_TIMEOUT);
 }
 
-template <int HD>
+template <int HD, int QR>
 cudaError_t launch_one(const PagedParams &p, const PagedMaps &tm, const PagedWork &w, int ctas, cudaStream_t st)
 {
-    using C = Shape<HD>;
+    using C = Shape<HD, QR>;
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = configure(paged_attend_tc_kernel<HD>, done, C::SMEM, false);
+    const cudaError_t e = configure(paged_attend_tc_kernel<HD, QR>, done, C::SMEM, false);
     if (e != cudaSuccess) return e;
-    return launch_kernel(p.early, paged_attend_tc_kernel<HD>, dim3(ctas), NTHREADS, C::SMEM, st, p, tm, w);
+    return launch_kernel(p.early, paged_attend_tc_kernel<HD, QR>, dim3(ctas), NTHREADS, C::SMEM, st, p, tm, w);
 }
 
 }  // namespace
@@ -449,11 +467,40 @@ bool page_map(const void *ptr, unsigned d, unsigned long long rows, unsigned box
 bool paged_tc_shape(const orthrus_paged_layer_t &L)
 {
     if (L.dtype != ORTHRUS_BF16 || (L.head_dim != 64 && L.head_dim != 128) || L.page_size < 16) return false;
+    const long long row_tiles = ((long long)L.n_q_heads / L.n_kv_heads * L.block + MROWS - 1) / MROWS;
+    if ((long long)L.batch * L.n_kv_heads * row_tiles * (((long long)L.max_pages * L.page_size + KT - 1) / KT) > 0x7fffffffLL) return false;
     return (unsigned long long)L.n_pages * L.n_kv_heads * L.page_size < 0x7fffffffull && tc_driver_ok();
 }
 
-// CTAs of a call, and what its workspace holds: from the shape and the host's bound on the lengths.
 namespace {
+
+int max_len_of(const orthrus_paged_layer_t &L)
+{
+    const long long n = L.max_len_hint > 0 ? (long long)L.max_len_hint : (long long)L.max_pages * L.page_size - L.block;
+    return n > 0 ? (int)n : 0;
+}
+
+// Which kernel.  Calls of up to 128 query rows a unit that take a few times as long as a launch go to the keys kernel (attend_keys.cu, over
+// pages), whose clusters meet through shared memory: CTAs per unit, or 0.  It gives every request as many CTAs as the longest may need; this
+// file's kernel shares the lengths out, and starts and joins in some 5 us more.  Us a call, here and there, 8 KV heads of 4 query heads:
+// one request of 2000, 4000, 16000, 32000 keys 10.7 and 5.8, 12.7 and 7.8, 23.9 and 20.2, 33.1 and 37.8; 8 of 500 to 4000 22.1 and
+// 20.9, of 1000 to 8000 32.1 and 39.4 (all of 8000 48 and 43); 32 of 125 to 1000 25.2 and 20.9, of 250 to 2000 34.1 and 39.1; blocks of 16, 8 of 500
+// to 4000 34.8 and 24.9, 4 of 2000 to 16000 56 and 44, 8 of those 68 and 83; one KV head, 16000 and 60000 keys 20.4 and 19.5, 42 and 67.
+// Hence: up to 200 MB of keys and values at the bound (270 MB where rows are many), one request any number, and up to 12 tiles a CTA.
+// ORTHRUS_TC_SMALL_ROWS=0 keeps all calls on this file's kernel, =1 puts there whatever fits (measurement knobs).
+int keys_plan(const orthrus_paged_layer_t &L)
+{
+    const int G = L.n_q_heads / L.n_kv_heads, knob = small_rows_knob();
+    if (knob == 0 || !keys_rows(L.head_dim, G, L.block)) return 0;
+    const int max_len = max_len_of(L), S = paged_keys_splits(L, max_len);
+    if (S == 0 || knob > 0) return S;
+    const int kb = keys_kb_rows(L.head_dim, G, L.block), tiles = (L.block + kb - 1) / kb;
+    const long long bytes = 4LL * L.head_dim * L.batch * L.n_kv_heads * tiles * max_len;
+    if (bytes > (G * L.block <= 16 ? 200000000LL : 270000000LL) && L.batch * tiles > 1) return 0;
+    return ((long long)max_len + L.block + KT - 1) / KT <= 24LL * S ? S : 0;
+}
+
+// CTAs of a call, and what its workspace holds: from the shape and the host's bound on the lengths.
 struct Grid { int ctas, row_tiles, rows, most_pieces; size_t counters, bytes; };
 Grid plan(const orthrus_paged_layer_t &L)
 {
@@ -462,13 +509,16 @@ Grid plan(const orthrus_paged_layer_t &L)
     g.row_tiles = (M + MROWS - 1) / MROWS;
     g.rows = M < MROWS ? M : MROWS;
     const long long units = (long long)L.batch * L.n_kv_heads * g.row_tiles;
-    const long long keys = (L.max_len_hint > 0 ? (long long)L.max_len_hint : (long long)L.max_pages * L.page_size - L.block) + L.block;
-    const long long tiles = units * (((keys < 1 ? 1 : keys) + KT - 1) / KT);
-    // Two CTAs an SM where there is much to stream; one where latency counts, which halves the pieces to join
-    const long long most = (tiles >= 16LL * num_sms() ? 2LL : 1LL) * num_sms();
+    const long long tiles = units * (((long long)max_len_of(L) + L.block + KT - 1) / KT);
+    // Two CTAs an SM; one where wide units are cut into more pieces than tiles are worth (8 KV heads, 8 requests of 2000 keys, 64 and 128
+    // rows 33.5 and 50 us at two, 30.5 and 40 at one; 4 rows 20.6 and 24.6; 32 requests of 1024 to 8192, 64 rows 111 and 147)
+    const long long most = (g.rows <= 16 || tiles >= 32LL * num_sms() ? 2LL : 1LL) * num_sms();
     g.ctas = (int)(tiles < 1 ? 1 : tiles < most ? tiles : most);
     // pieces of a unit: what the join has room for, and no more than one CTA adds up in the time the others save
-    const int room = (L.head_dim == 128 ? Shape<128>::JOIN : Shape<64>::JOIN) / (g.rows * 8);
+    int padded = 1;
+    while (padded < g.rows) padded *= 2;
+    const int room = (L.head_dim == 128 ? g.rows <= 64 ? Shape<128, 64>::JOIN : Shape<128, 128>::JOIN
+                                        : g.rows <= 64 ? Shape<64, 64>::JOIN : Shape<64, 128>::JOIN) / (padded * 8);
     g.most_pieces = room < 32 ? room : 32;
     g.counters = (size_t)((units * 4 + 255) / 256 * 256);
     g.bytes = g.counters + 2 * (size_t)g.ctas * piece_floats(g.rows, L.head_dim) * sizeof(float);
@@ -480,10 +530,7 @@ size_t paged_tc_workspace_bytes(const orthrus_paged_layer_t &L) { return plan(L)
 
 cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_layer_t &L, void *ws_body, cudaStream_t st)
 {
-    const int max_len = L.max_len_hint > 0 ? L.max_len_hint : p.max_pos > p.K ? p.max_pos - p.K : 0;
-    const int S = paged_keys_splits(L, max_len);
-    const char *pk = getenv("PK");
-    if (S > 0 && pk && pk[0] == '1') return launch_paged_attend_keys(p, S, st);
+    if (const int S = keys_plan(L)) return launch_paged_attend_keys(p, S, st);
     const Grid g = plan(L);
     PagedWork w;
     w.row_tiles = g.row_tiles;
@@ -496,7 +543,8 @@ cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_lay
     const unsigned long long rows = (unsigned long long)L.n_pages * L.n_kv_heads * L.page_size;
     if (!page_map(p.k_pages, p.d, rows, 1u << w.box_shift, &tm.k) || !page_map(p.v_pages, p.d, rows, 1u << w.box_shift, &tm.v))
         return cudaErrorInvalidValue;
-    return p.d == 128 ? launch_one<128>(p, tm, w, g.ctas, st) : launch_one<64>(p, tm, w, g.ctas, st);
+    if (p.d == 128) return g.rows <= 64 ? launch_one<128, 64>(p, tm, w, g.ctas, st) : launch_one<128, 128>(p, tm, w, g.ctas, st);
+    return g.rows <= 64 ? launch_one<64, 64>(p, tm, w, g.ctas, st) : launch_one<64, 128>(p, tm, w, g.ctas, st);
 }
 
 }  // namespace orthrus

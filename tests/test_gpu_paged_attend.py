@@ -11,6 +11,14 @@ pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
 
 
+@pytest.fixture(params=["by the rule", "0", "1"], autouse=True)
+def kernel(request, monkeypatch):
+    """Few rows run on either tensor-core kernel: as the rule has it, on the one that shares lengths out, on the keys kernel where it fits."""
+    monkeypatch.delenv("ORTHRUS_TC_SMALL_ROWS", raising=False)
+    if request.param in ("0", "1"):
+        monkeypatch.setenv("ORTHRUS_TC_SMALL_ROWS", request.param)
+
+
 def make(B, K, Hq, Hkv, d, page, dtype, lens, new, seed=1, spare_width=0, q_scale=1.0):
     """Pages dealt at random; whatever no row of a request occupies is NaN, and table entries that no row needs are outside the pool."""
     g = torch.Generator().manual_seed(seed)
