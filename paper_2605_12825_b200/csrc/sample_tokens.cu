@@ -2,20 +2,23 @@
 //
 // Every filter cuts the row, ordered by value falling and id rising, at one place; so does the draw.  A place is a value and a count of
 // the ties at it, so that no sorting is needed: it is enough to know, for the values in order, how many tokens have them and what they weigh.
-//   1. A cluster of CTAs counts its row's values in shared memory, one pass over the logits.  bf16 has few values: those with magnitude
-//      2^-20 to 2^8 and zero have a bin each, what is outside shares four.  Weights are then needed once per value and not once per token (an
-//      exponential in double precision for a few thousand values instead of 150 thousand tokens).  fp32: bins of 2^20 neighbouring
-//      values, which carry counts and the sum of their tokens' weights; the maximum is found by a pass before.
+//   1. A CTA (few rows: a cluster) counts its row's values in shared memory, one pass over the logits.  bf16 has few values: those with
+//      magnitude 2^-24 to 2^8 and zero have a bin each, what is outside shares four.  Weights are then needed once per value and not once per
+//      token (an exponential in double precision for a few thousand values instead of 150 thousand tokens).  fp32: bins of 2^16 neighbouring
+//      values, magnitudes 2^-8 to 2^8, which carry counts and the sum of their tokens' weights; the maximum is found by a pass before.
 //   2. Sums over groups of 32 bins go to one CTA, which finds the bin of each cut from them.
-//   3. A cut in a bin of many values: another pass counts and weighs 1024 parts of that bin, until a part is one value.
-//   4. The CTA that holds the wanted occurrence of the drawn value finds its id.
-// Weights are integers, exp((x - max) / T) in steps of 2^-S with 2^S times the vocabulary below 2^63: sums do not depend on the
+//   3. A cut in a bin of many values: another pass lists the bin's tokens, which are ranked; if there are too many, it counts and weighs 1024
+//      parts of the bin, until a part is one value.
+//   4. The wanted occurrence of the drawn value: a pass marks them in a bit map.
+// Weights are integers, exp((x - max) / T) in steps of 2^-S with 2^S times the vocabulary at most 2^62: sums do not depend on the
 // order in which atomics arrive, are exact, and a border is off by no more than the weights' own rounding.
 //
-// What bounds it: one row, latency (five dependent steps at the cluster's barriers); many rows, the atomics in shared memory (one a
-// token for bf16, three for fp32 next to an exponential in double).
+// What bounds it: one row, latency (its steps follow one another at the cluster's barriers); many rows, the atomics in shared memory (one
+// a token for bf16, three for fp32 next to an exponential in double).
 #include <cooperative_groups.h>
 #include <cmath>
+#include <cstddef>
+#include <type_traits>
 #include "paged.cuh"
 #include "tc_ptx.cuh"
 
@@ -24,71 +27,47 @@ namespace cg = cooperative_groups;
 namespace orthrus {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kParts = 1024;                       // parts of a bin that a cut falls into
+constexpr int kParts = 1024;                       // parts of a bin that a cut falls into, or tokens of one that are listed
 constexpr uint32_t kNone = 0xffffffffu;            // no candidate: NaN, -inf
 
-// Values as whole numbers that rise as the value falls; -0 is 0.  Bins of neighbouring ones.
-template <typename T> struct Keys;
-template <> struct Keys<__nv_bfloat16> {
-    static constexpr int N = 8;                                        // elements of 16 bytes
-    static constexpr uint32_t LO = 107u << 7, HI = 135u << 7;          // magnitudes 2^-20 and 2^8
-    static constexpr int FINE = HI - LO, BINS = 2 * FINE + 5, STEPS = (BINS + 31) / 32, WEIGHED = 4;
-    using Raw = uint16_t;
-    __device__ static uint32_t key(uint32_t h) {                       // h: the 16 bits
-        const uint32_t mag = h & 0x7fff;
-        if (mag >= 0x7f80 && h != 0x7f80) return kNone;
-        return mag == 0 || !(h & 0x8000) ? 0x7fff - mag : 0x8000 + mag;
+// Values as whole numbers that rise as the value falls (keys); -0 is 0.  Bins of neighbouring ones, by the 16 leading bits: FINE for each
+// sign, one for zero, and four wide ones: above, below and (either sign) near zero.
+template <typename T> struct Keys {
+    static constexpr bool HALF = sizeof(T) == 2;
+    static constexpr int N = 16 / sizeof(T);                           // elements of 16 bytes
+    static constexpr uint32_t LO = (HALF ? 103u : 119u) << 7, HI = 135u << 7;      // magnitudes 2^-24 or 2^-8, and 2^8
+    static constexpr int FINE = HI - LO, BINS = 2 * FINE + 5, STEPS = (BINS + 31) / 32, WEIGHED = HALF ? 4 : BINS;
+    static constexpr int LOW = HALF ? 0 : 16;                          // bits behind the leading 16
+    static constexpr uint32_t SIGN = HALF ? 0x8000u : 0x80000000u, INF = 0x7f80u << LOW;
+    using Raw = std::conditional_t<HALF, uint16_t, uint32_t>;
+    __device__ static uint32_t key(uint32_t h) {                       // h: the bits
+        const uint32_t mag = h & (SIGN - 1);
+        if (mag >= INF && h != INF) return kNone;
+        return mag == 0 || !(h & SIGN) ? SIGN - 1 - mag : h;
     }
-    __device__ static double value(uint32_t d) {
-        const uint32_t h = d <= 0x7fff ? 0x7fff - d : d;               // (0x8000 + mag are the bits themselves)
-        return (double)__uint_as_float(h << 16);
-    }
+    __device__ static uint32_t bits(uint32_t d) { return d < SIGN ? SIGN - 1 - d : d; }
+    __device__ static double value(uint32_t d) { return (double)__uint_as_float(bits(d) << (16 - LOW)); }
     __device__ static int bin(uint32_t d) {
-        if (d == 0x7fff) return FINE + 2;
-        const uint32_t mag = d < 0x7fff ? 0x7fff - d : d - 0x8000;
+        if (d == SIGN - 1) return FINE + 2;
+        const uint32_t mag = (d < SIGN ? SIGN - 1 - d : d - SIGN) >> LOW;
         const int t = (int)(min(max(mag, LO - 1), HI) - (LO - 1));
-        return d < 0x7fff ? FINE + 1 - t : FINE + 3 + t;
+        return d < SIGN ? FINE + 1 - t : FINE + 3 + t;
     }
-    // the bin of an element, straight from its bits; < 0: no candidate
-    __device__ static int bin_of(uint32_t h) {
-        const uint32_t mag = h & 0x7fff;
-        const int t = (int)(min(max(mag, LO - 1), HI) - (LO - 1));
-        int b = h & 0x8000 ? FINE + 3 + t : FINE + 1 - t;
-        if (mag - 1 >= 0x7f7f) b = mag == 0 ? FINE + 2 : h == 0x7f80 ? 0 : -1;
-        return b;
-    }
-    // first value of a bin; which of the bins of many values it is (-1: it is one value)
+    static constexpr int ZERO = FINE + 2;
+    __device__ static bool wide(int b) { return b == 0 || b == FINE + 1 || b == FINE + 3 || b == BINS - 1; }
+    __device__ static bool one_value(int b) { return HALF && !wide(b); }
+    __device__ static int weighed(int b) { return HALF ? (b == 0 ? 0 : b == FINE + 1 ? 1 : b == FINE + 3 ? 2 : 3) : b; }      // where its mass is
+    // log2 of how many keys a bin has at most, and the first
+    __device__ static int width(int b) { return wide(b) ? HALF ? 15 : 30 : LOW; }
     __device__ static uint32_t first(int b) {
+        const uint32_t more = (1u << LOW) - 1;
         if (b == 0) return 0;
-        if (b <= FINE) return 0x7fff - (HI - b);
-        if (b == FINE + 1) return 0x7fff - (LO - 1);
-        if (b == FINE + 2) return 0x7fff;
-        if (b == FINE + 3) return 0x8001;
-        return 0x8000 + LO + (uint32_t)(b - FINE - 4);
+        if (b <= FINE) return SIGN - 1 - ((HI - b) << LOW | more);
+        if (b == FINE + 1) return SIGN - 1 - (((LO - 1) << LOW) | more);
+        if (b == ZERO) return SIGN - 1;
+        if (b == FINE + 3) return SIGN + 1;
+        return SIGN + ((LO + (uint32_t)(b - FINE - 4)) << LOW);
     }
-    __device__ static int weighed(int b) { return b == 0 ? 0 : b == FINE + 1 ? 1 : b == FINE + 3 ? 2 : b == BINS - 1 ? 3 : -1; }
-    static constexpr int BITS = 15;                                     // a bin has at most 2^BITS values
-    template <class F> __device__ static void each(const uint4 &u, F f) {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { f(2 * k, w[k] & 0xffffu); f(2 * k + 1, w[k] >> 16); }
-    }
-};
-template <> struct Keys<float> {
-    static constexpr int N = 4;
-    static constexpr int BITS = 20, BINS = 4096, STEPS = BINS / 32, WEIGHED = BINS;
-    using Raw = uint32_t;
-    __device__ static uint32_t key(uint32_t h) {
-        const uint32_t mag = h & 0x7fffffffu;
-        if (mag >= 0x7f800000u && h != 0x7f800000u) return kNone;
-        return mag == 0 || !(h >> 31) ? 0x7fffffffu - mag : h;
-    }
-    __device__ static double value(uint32_t d) { return (double)__uint_as_float(d <= 0x7fffffffu ? 0x7fffffffu - d : d); }
-    __device__ static int bin(uint32_t d) { return (int)(d >> BITS); }
-    __device__ static uint32_t first(int b) { return (uint32_t)b << BITS; }
-    __device__ static int weighed(int b) { return b; }
-    template <class F> __device__ static void each(const uint4 &u, F f) { f(0, u.x); f(1, u.y); f(2, u.z); f(3, u.w); }
 };
 
 struct SampleArgs {
@@ -101,6 +80,31 @@ struct SampleArgs {
     float *logprob;
 };
 
+// 2^(j / 32)
+__constant__ double kTwoTo[32] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0,
+};
+// e^x for x <= 0, to a few units of 2^-53: x = n (ln 2 / 32) + r, the Taylor polynomial of degree 6 in r (its remainder is below 2^-57), times
+// 2^(n mod 32 / 32), and n / 32 added to the exponent.  (Below -700, and of NaN: 0.)  Here because the fp64 pipe is what the sums over bins
+// wait for, and this is half the instructions of a polynomial without a table (512 rows of 128256: 16 us of a call, and SUMS us).
+__device__ inline double exp_of(double x, const double *two_to)
+{
+    const double n = rint(fmax(x, -800.0) * 46.166241308446828384);       // (NaN: -800)
+    const double r = fma(n, -7.247021293269686e-19, fma(n, -0.02166084939249829, x));                      // (ln 2 / 32 as a double, and what it lacks)
+    const int k = (int)n;
+    double y = 1.0 / 720.0;
+    y = fma(y, r, 1.0 / 120.0); y = fma(y, r, 1.0 / 24.0); y = fma(y, r, 1.0 / 6.0); y = fma(y, r, 0.5); y = fma(y, r, 1.0); y = fma(y, r, 1.0);
+    y *= two_to[k & 31];
+    return x > -700.0 ? __hiloint2double(__double2hiint(y) + ((k >> 5) << 20), __double2loint(y)) : 0.0;
+}
+
 // A sum of 64 bits as two of 32 that atomics can add to
 struct Sum { uint32_t lo, hi; };
 __device__ inline void add_to(Sum *s, unsigned long long x) {
@@ -109,24 +113,39 @@ __device__ inline void add_to(Sum *s, unsigned long long x) {
 }
 __device__ inline unsigned long long whole(const Sum &s) { return (unsigned long long)s.hi << 32 | s.lo; }
 
-// A place in the order: token number `tie` (from 0) of those with key d, which weigh w each; before it, and by its CTAs
-struct Place { uint32_t d, tie, count_before, owner, owner_tie; int bin; unsigned long long mass_before, w; };
+// A place in the order: token number `tie` (from 0) of those with key d, which weigh w each; what is before them; its id, where that is known
+struct Place { uint32_t d, tie, count_before, count_at, id; int bin; unsigned long long mass_before, w; };
 
+constexpr int kPartSteps = kParts / 32;
 template <typename T> struct Shared {
-    uint32_t count[Keys<T>::STEPS * 32];
+    uint32_t count[Keys<T>::STEPS * 32];                 // (in the end: the bit map)
     Sum mass[Keys<T>::WEIGHED];
-    uint32_t part_count[kParts];
-    Sum part_mass[kParts];
-    unsigned long long step_mass[Keys<T>::STEPS + 1];    // CTA 0: sums of the groups of 32 bins, then of all before
-    uint32_t step_count[Keys<T>::STEPS + 1];
-    unsigned long long part_step_mass[kParts / 32 + 1];  // likewise for the parts
-    uint32_t part_step_count[kParts / 32 + 1];
+    union {
+        struct { uint32_t count[kParts]; Sum mass[kParts]; } part;
+        struct { uint32_t key[kParts], id[kParts]; unsigned long long w[kParts]; } list;
+        uint32_t wide_bits[4 * kParts];                  // first pass over bf16: bits of tokens in the wide bins
+    };
+    // CTA 0: sums of the groups of 32 bins, then of all before; behind them those of the parts
+    unsigned long long step_mass[Keys<T>::STEPS + 1 + kPartSteps + 1];
+    uint32_t step_count[Keys<T>::STEPS + 1 + kPartSteps + 1];
     Place place;
-    uint32_t top, per_warp[kWarps];
+    uint32_t top, found, per_warp[16];
+    double two_to[32];                                   // 2^(j / 32)
+    // CTA 0 of several: what all of them have counted (a launch of single CTAs leaves out the room for these)
+    uint32_t all_count[Keys<T>::STEPS * 32];
+    Sum all_mass[Keys<T>::WEIGHED];
 };
 
 enum Mode { BY_COUNT, BY_MASS, BY_KEY };
 
+__device__ inline uint32_t scan_sum(uint32_t x, int lane) {
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+    }
+    return x;
+}
 __device__ inline unsigned long long scan_sum(unsigned long long x, int lane) {
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -136,145 +155,205 @@ __device__ inline unsigned long long scan_sum(unsigned long long x, int lane) {
     return x;
 }
 
-template <typename T>
+// sum over a warp, of numbers below 2^63 whose sum is
+__device__ inline unsigned long long warp_total(unsigned long long x) {
+    const unsigned long long lo = __reduce_add_sync(0xffffffffu, (uint32_t)x & 0xffffff), mid = __reduce_add_sync(0xffffffffu, (uint32_t)(x >> 24) & 0xffffff),
+                             hi = __reduce_add_sync(0xffffffffu, (uint32_t)(x >> 48));
+    return lo + (mid << 24) + (hi << 48);
+}
+
+template <typename T, int kThreads>
 struct Sampler {
     using K = Keys<T>;
+    static constexpr int kWarps = kThreads / 32;
     Shared<T> &sh;
     const SampleArgs &a;
     cg::cluster_group cluster;
     const T *row;
     int tid, lane, warp, C, rank;
-    int skew, n_vec, v0, v1;               // vector v: elements [v N - skew, v N - skew + N); this CTA's vectors
+    int e0, e1;                            // this CTA's elements
     uint32_t top;                          // key of the largest
     double x_top, inv_t, scale;
 
     __device__ void meet() { if (C > 1) cluster.sync(); else __syncthreads(); }
     __device__ Shared<T> *of(int r) { return C > 1 ? cluster.map_shared_rank(&sh, r) : &sh; }
     __device__ double share(uint32_t d) const {            // exp((x - max) / T)
-        if (d == top) return 1.0;
-        const double y = K::value(d) - x_top;
-        return y == -INFINITY ? 0.0 : exp(y * inv_t);
+        return d == top ? 1.0 : exp_of((K::value(d) - x_top) * inv_t, sh.two_to);
     }
     __device__ unsigned long long weight(uint32_t d) const { return __double2ull_rn(share(d) * scale); }
 
-    // f(element, bits) for the elements of vectors [b, e), lanes and warps (or one warp's lanes) side by side
-    template <class F> __device__ void elements(int b, int e, int at, int step, F f) const {
-        const uint4 *vec = reinterpret_cast<const uint4 *>(row - skew);
-        int v = b + at;
-        auto part = [&](int v) {
-            const int i0 = v * K::N - skew;
-            for (int k = max(0, -i0); k < min(K::N, a.vocab - i0); ++k) f(i0 + k, (uint32_t)reinterpret_cast<const typename K::Raw *>(row)[i0 + k]);
-        };
-        auto is_whole = [&](int v) { return v * K::N >= skew && v * K::N - skew + K::N <= a.vocab; };
-        for (; v + 3 * step < e; v += 4 * step) {
-            if (is_whole(v) && is_whole(v + 3 * step)) {
-                uint4 u[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) u[q] = __ldg(vec + v + q * step);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) K::each(u[q], [&](int k, uint32_t h) { f((v + q * step) * K::N - skew + k, h); });
-            } else {
+    // f(element, 16 bytes) for the whole vectors among elements [b, e), U loads of a thread under way together; g(element, bits) for the
+    // elements in front of and behind them
+    template <int U, class F, class G> __device__ void vectors(int b, int e, F f, G g) const {
+        const int skew = (int)((reinterpret_cast<uintptr_t>(row + b) & 15) / sizeof(T)), head = min((K::N - skew) % K::N, e - b);
+        const int n = (e - b - head) / K::N, tail = b + head + n * K::N;
+        const uint4 *x = reinterpret_cast<const uint4 *>(row + b + head);
+        int v = tid;
 #pragma unroll 1
-                for (int q = 0; q < 4; ++q) {
-                    if (is_whole(v + q * step)) {
-                        const uint4 u = __ldg(vec + v + q * step);
-                        K::each(u, [&](int k, uint32_t h) { f((v + q * step) * K::N - skew + k, h); });
-                    } else part(v + q * step);
-                }
-            }
+        for (; v + (U - 1) * kThreads < n; v += U * kThreads) {
+            uint4 u[U];
+#pragma unroll
+            for (int q = 0; q < U; ++q) u[q] = __ldg(x + v + q * kThreads);
+#pragma unroll
+            for (int q = 0; q < U; ++q) f(b + head + (v + q * kThreads) * K::N, u[q]);
         }
-        for (; v < e; v += step) {
-            if (is_whole(v)) {
-                const uint4 u = __ldg(vec + v);
-                K::each(u, [&](int k, uint32_t h) { f(v * K::N - skew + k, h); });
-            } else part(v);
-        }
+        if (U > 1)
+#pragma unroll 1
+            for (; v < n; v += kThreads) f(b + head + v * K::N, __ldg(x + v));
+        // (at most N - 1 each, fewer than the threads)
+        const int i = tid < head ? b + tid : tid - head < e - tail ? tail + tid - head : -1;
+        if (i >= 0) g(i, (uint32_t)__ldg(reinterpret_cast<const typename K::Raw *>(row) + i));
     }
-    template <class F> __device__ void mine(F f) const { elements(v0, v1, tid, kThreads, f); }
+    // f(element, bits) for this CTA's elements.  In little code: for what is not done for every row
+    template <class F> __device__ void mine(F f) const {
+        vectors<4>(e0, e1,
+                [&](int i0, uint4 u) {
+#pragma unroll 1
+                    for (int k = 0; k < K::N; ++k) {
+                        f(i0 + k, K::HALF ? u.x & 0xffff : u.x);
+                        if (K::HALF) { u.x = __funnelshift_r(u.x, u.y, 16); u.y = __funnelshift_r(u.y, u.z, 16); u.z = __funnelshift_r(u.z, u.w, 16); u.w >>= 16; }
+                        else { u.x = u.y; u.y = u.z; u.z = u.w; }
+                    }
+                },
+                f);
+    }
 
-    // key of the row's largest, known to every CTA; the barriers of a cluster
+    // key of the row's largest, from every CTA's (sh.top, before a barrier)
+    __device__ uint32_t top_of_all() {
+        const uint32_t x = lane < C ? of(lane)->top : kNone;
+        return __reduce_min_sync(0xffffffffu, x);
+    }
     __device__ void find_top() {
-        if (tid == 0) sh.top = kNone;
-        __syncthreads();
         uint32_t best = kNone;
         mine([&](int, uint32_t h) { best = min(best, K::key(h)); });
         best = __reduce_min_sync(0xffffffffu, best);
         if (lane == 0) atomicMin(&sh.top, best);
-        meet();
-        top = sh.top;
-        for (int r = 0; r < C; ++r) top = min(top, of(r)->top);
-        meet();
     }
 
-    // merged count and mass of a bin (or of a part of one); `d`: its first value, `one`: it has no other
-    __device__ void merged(bool parts, int b, uint32_t d, bool one, uint32_t &count, unsigned long long &mass) {
-        count = 0; mass = 0;
-        const int m = parts ? b : K::weighed(b);
-        for (int r = 0; r < C; ++r) {
-            const Shared<T> *s = of(r);
-            count += parts ? s->part_count[b] : s->count[b];
-            if (!one) mass += whole(parts ? s->part_mass[b] : s->mass[m]);
-        }
-        if (one && count) mass = count * weight(d);
+    // what is in bin b, of parts if `parts`, by its first value d (`one`: it has no other)
+    __device__ void in_bin(bool parts, int b, uint32_t d, bool one, uint32_t &count, unsigned long long &mass) {
+        count = parts ? sh.part.count[b] : C > 1 ? sh.all_count[b] : sh.count[b];
+        mass = 0;
+        if (one) { if (count) mass = count * weight(d); }
+        else mass = whole(parts ? sh.part.mass[b] : C > 1 ? sh.all_mass[K::weighed(b)] : sh.mass[K::weighed(b)]);
     }
-    // sums of groups of 32 bins to CTA 0 (groups shared out over warps and CTAs)
+    // Sums of groups of 32 bins to CTA 0, and, where there are several CTAs, of the bins themselves; groups shared out over warps and CTAs, two
+    // at a time, whose exponentials run side by side.
     __device__ void sum_steps() {
         Shared<T> *to = of(0);
-        for (int s = rank * kWarps + warp; s < K::STEPS; s += C * kWarps) {
-            const int b = s * 32 + lane;
-            uint32_t count = 0;
-            unsigned long long mass = 0;
-            if (b < K::BINS) merged(false, b, K::first(b), K::weighed(b) < 0, count, mass);
-            count = __reduce_add_sync(0xffffffffu, count);
-            if (count) mass = __shfl_sync(0xffffffffu, scan_sum(mass, lane), 31);
-            if (lane == 0) { to->step_count[s] = count; to->step_mass[s] = count ? mass : 0; }
+        constexpr int U = 2;
+#pragma unroll 1
+        for (int s0 = rank * kWarps + warp; s0 < K::STEPS; s0 += U * C * kWarps) {
+            uint32_t count[U];
+            unsigned long long mass[U];
+            bool one[U], wide[U];
+            int b[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int s = s0 + k * C * kWarps;
+                b[k] = min(s * 32 + lane, K::STEPS * 32 - 1);
+                const bool is = s < K::STEPS && b[k] < K::BINS;
+                one[k] = is && K::one_value(b[k]);
+                wide[k] = is && !one[k];
+                count[k] = 0;
+                mass[k] = 0;
+                if (C == 1) {
+                    if (is) count[k] = sh.count[b[k]];
+                    if (wide[k]) mass[k] = whole(sh.mass[K::weighed(b[k])]);
+                } else {
+                    const Sum *m = sh.mass + (wide[k] ? K::weighed(b[k]) : 0);
+                    uint32_t x[8];
+                    Sum y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {              // (at most eight CTAs)
+                        x[i] = is && i < C ? *cluster.map_shared_rank(sh.count + b[k], i) : 0;
+                        y[i] = wide[k] && i < C ? *cluster.map_shared_rank(m, i) : Sum{0, 0};
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { count[k] += x[i]; mass[k] += whole(y[i]); }
+                    if (is) to->all_count[b[k]] = count[k];
+                    if (wide[k]) to->all_mass[K::weighed(b[k])] = Sum{(uint32_t)mass[k], (uint32_t)(mass[k] >> 32)};
+                }
+            }
+            if (K::HALF && __any_sync(0xffffffffu, count[0] | count[U - 1])) {
+                unsigned long long w[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) w[k] = weight(K::first(min(b[k], K::BINS - 1)));
+#pragma unroll
+                for (int k = 0; k < U; ++k) if (one[k]) mass[k] = count[k] * w[k];
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int s = s0 + k * C * kWarps;
+                const uint32_t n = __reduce_add_sync(0xffffffffu, count[k]);
+                unsigned long long m = 0;
+                if (n) m = warp_total(mass[k]);
+                if (lane == 0 && s < K::STEPS) { to->step_count[s] = n; to->step_mass[s] = m; }
+            }
         }
     }
-    // sums of groups become sums of all groups before; by one warp
-    __device__ void run_steps(uint32_t *count, unsigned long long *mass, int n) {
-        unsigned long long c_run = 0, m_run = 0;
-        for (int s0 = 0; s0 < n; s0 += 32) {
-            const int s = s0 + lane;
-            const unsigned long long c = s < n ? count[s] : 0, m = s < n ? mass[s] : 0;
-            const unsigned long long ci = scan_sum(c, lane), mi = scan_sum(m, lane);
-            if (s < n) { count[s] = (uint32_t)(c_run + ci - c); mass[s] = m_run + mi - m; }
-            c_run += __shfl_sync(0xffffffffu, ci, 31);
-            m_run += __shfl_sync(0xffffffffu, mi, 31);
+    // the same for the parts, all of which are CTA 0's
+    __device__ void sum_parts(uint32_t base, int shift) {
+#pragma unroll 1
+        for (int s = warp; s < kPartSteps; s += kWarps) {
+            uint32_t count;
+            unsigned long long mass;
+            in_bin(true, s * 32 + lane, base + ((uint32_t)(s * 32 + lane) << shift), shift == 0, count, mass);
+            count = __reduce_add_sync(0xffffffffu, count);
+            mass = warp_total(mass);
+            if (lane == 0) { sh.step_count[K::STEPS + 1 + s] = count; sh.step_mass[K::STEPS + 1 + s] = mass; }
         }
-        if (lane == 0) { count[n] = (uint32_t)c_run; mass[n] = m_run; }
+    }
+    // sums of groups become sums of all groups before, in place, the total behind them; by one warp of CTA 0
+    __device__ void run_steps(bool parts) {
+        const int n = parts ? kPartSteps : K::STEPS;
+        uint32_t *count = sh.step_count + (parts ? K::STEPS + 1 : 0);
+        unsigned long long *mass = sh.step_mass + (parts ? K::STEPS + 1 : 0);
+        const int per = (n + 31) / 32, b = min(n, lane * per), e = min(n, b + per);
+        uint32_t c = 0;
+        unsigned long long m = 0;
+        for (int s = b; s < e; ++s) { c += count[s]; m += mass[s]; }
+        uint32_t cr = scan_sum(c, lane) - c;
+        unsigned long long mr = scan_sum(m, lane) - m;
+        for (int s = b; s < e; ++s) {
+            const uint32_t x = count[s];
+            const unsigned long long y = mass[s];
+            count[s] = cr; mass[s] = mr;
+            cr += x; mr += y;
+        }
+        if (lane == 31) { count[n] = cr; mass[n] = mr; }
         __syncwarp();
     }
     // By one warp of CTA 0: the bin (or part) in which the running count or mass passes y, or which holds the key y.  p.count_before and
     // p.mass_before: of all before the bins at hand.
-    __device__ void search(bool parts, Mode mode, unsigned long long y, int shift, uint32_t base, Place &p, uint32_t &count_at) {
-        const uint32_t *sc = parts ? sh.part_step_count : sh.step_count;
-        const unsigned long long *sm = parts ? sh.part_step_mass : sh.step_mass;
-        const int n = parts ? kParts / 32 : K::STEPS;
-        int s = 0;
-        if (mode == BY_KEY) s = (parts ? (int)(((uint32_t)y - base) >> shift) : K::bin((uint32_t)y)) >> 5;
-        else
-            for (int s0 = 0; s0 < n; s0 += 32) {
-                const int i = s0 + lane;
-                const bool below = i < n && (mode == BY_COUNT ? p.count_before + (unsigned long long)sc[i + 1] <= y : p.mass_before + sm[i + 1] <= y);
-                s += __popc(__ballot_sync(0xffffffffu, below));
-            }
-        s = min(s, n - 1);
+    __device__ void search(bool parts, Mode mode, unsigned long long y, int shift, uint32_t base, Place &p) {
+        const uint32_t *sc = sh.step_count + (parts ? K::STEPS + 1 : 0);
+        const unsigned long long *sm = sh.step_mass + (parts ? K::STEPS + 1 : 0);
+        const int n = parts ? kPartSteps : K::STEPS;
+        const int by_key = parts ? (int)(((uint32_t)y - base) >> shift) : K::bin((uint32_t)y);       // (of BY_KEY)
+        int s = by_key >> 5;
+        if (mode != BY_KEY) {
+            uint32_t below = 0;
+#pragma unroll 4
+            for (int i = lane; i < n; i += 32)
+                below += mode == BY_COUNT ? p.count_before + (unsigned long long)sc[i + 1] <= y : p.mass_before + sm[i + 1] <= y;
+            s = min((int)__reduce_add_sync(0xffffffffu, below), n - 1);
+        }
         const int b = s * 32 + lane;
         const uint32_t d = parts ? base + ((uint32_t)b << shift) : b < K::BINS ? K::first(b) : kNone;
         uint32_t count = 0;
         unsigned long long mass = 0;
-        if (parts || b < K::BINS) merged(parts, b, d, parts ? shift == 0 : K::weighed(b) < 0, count, mass);
-        const unsigned long long ci = scan_sum(count, lane), mi = scan_sum(mass, lane);
-        const unsigned long long cb = p.count_before + sc[s] + ci - count, mb = p.mass_before + sm[s] + mi - mass;
-        unsigned hit;
-        if (mode == BY_KEY) hit = 1u << ((parts ? (int)(((uint32_t)y - base) >> shift) : K::bin((uint32_t)y)) & 31);
-        else hit = __ballot_sync(0xffffffffu, mode == BY_COUNT ? cb + count > y : mb + mass > y);
+        if (parts || b < K::BINS) in_bin(parts, b, d, parts ? shift == 0 : K::one_value(b), count, mass);
+        const uint32_t cb = p.count_before + sc[s] + scan_sum(count, lane) - count;
+        const unsigned long long mb = p.mass_before + sm[s] + scan_sum(mass, lane) - mass;
+        const unsigned hit = mode == BY_KEY ? 1u << (by_key & 31)
+                                            : __ballot_sync(0xffffffffu, mode == BY_COUNT ? (unsigned long long)cb + count > y : mb + mass > y);
         const int l = hit ? __ffs(hit) - 1 : 31;
         p.bin = __shfl_sync(0xffffffffu, b, l);
         p.d = __shfl_sync(0xffffffffu, d, l);
-        p.count_before = (uint32_t)__shfl_sync(0xffffffffu, cb, l);
+        p.count_before = __shfl_sync(0xffffffffu, cb, l);
         p.mass_before = __shfl_sync(0xffffffffu, mb, l);
-        count_at = __shfl_sync(0xffffffffu, count, l);
+        p.count_at = __shfl_sync(0xffffffffu, count, l);
     }
 
     // The place where the running count or mass passes y, or behind the last token with key at most y (BY_KEY).  All CTAs call it
@@ -285,63 +364,105 @@ struct Sampler {
         bool parts = false;
         int shift = 0;
         uint32_t base = 0;
+#pragma unroll 1
         for (;;) {
             if (rank == 0 && warp == 0) {
-                uint32_t count_at;
-                search(parts, mode, y, shift, base, p, count_at);
-                const bool one = parts ? shift == 0 : K::weighed(p.bin) < 0;
+                if (parts) run_steps(true);
+                search(parts, mode, y, shift, base, p);
+                const bool one = parts ? shift == 0 : K::one_value(p.bin);
                 p.w = one ? weight(p.d) : 0;
-                p.tie = p.owner = p.owner_tie = 0;
+                p.id = kNone;
+                // which of the tokens with this key
+                p.tie = 0;
                 if (one) {
-                    // which of the tokens with this key, and whose it is
                     if (mode == BY_COUNT) p.tie = (uint32_t)(y - p.count_before);
-                    else if (mode == BY_MASS) p.tie = p.w ? (uint32_t)min((y - p.mass_before) / p.w, (unsigned long long)count_at - 1) : 0;
-                    else p.tie = count_at;                                // (one behind the last of them)
-                    const uint32_t c = lane < C ? (parts ? of(lane)->part_count[p.bin] : of(lane)->count[p.bin]) : 0;
-                    const uint32_t upto = (uint32_t)scan_sum(c, lane);
-                    const unsigned hit = __ballot_sync(0xffffffffu, upto > p.tie);
-                    p.owner = hit ? __ffs(hit) - 1 : 0;
-                    p.owner_tie = p.tie - __shfl_sync(0xffffffffu, upto - c, p.owner);
+                    else if (mode == BY_MASS) p.tie = p.w ? (uint32_t)min((y - p.mass_before) / p.w, (unsigned long long)p.count_at - 1) : 0;
+                    else p.tie = p.count_at;                              // (one behind the last of them)
                 }
                 if (lane < C) of(lane)->place = p;
+                if (lane == 0) sh.found = 0;
             }
             meet();
             p = sh.place;
-            const bool one = parts ? shift == 0 : K::weighed(p.bin) < 0;
-            if (one) { meet(); return p; }
+            if (parts ? shift == 0 : K::one_value(p.bin)) { meet(); return p; }
+            if (!parts && p.count_at <= kParts) return ranked(mode, y, p);
             // the bin's parts
             base = p.d;
-            shift = parts ? max(0, shift - 10) : max(0, K::BITS - 10);
+            shift = max(0, (parts ? shift : K::width(p.bin)) - 10);
             parts = true;
-            for (int i = tid; i < kParts; i += kThreads) { sh.part_count[i] = 0; sh.part_mass[i] = Sum{0, 0}; }
+            for (int i = tid; i < kParts; i += kThreads) { sh.part.count[i] = 0; sh.part.mass[i] = Sum{0, 0}; }
             __syncthreads();
-            const int keep = shift;
             mine([&](int, uint32_t h) {
-                const uint32_t d = K::key(h), off = (d - base) >> keep;
+                const uint32_t d = K::key(h), off = (d - base) >> shift;
                 if (d != kNone && d >= base && off < kParts) {
-                    atomicAdd(&sh.part_count[off], 1u);
-                    if (keep) add_to(&sh.part_mass[off], weight(d));
+                    atomicAdd(&sh.part.count[off], 1u);
+                    if (shift) add_to(&sh.part.mass[off], weight(d));
                 }
             });
+            if (C > 1) {
+                // to those of CTA 0 (few are not empty: the bin was one of thousands)
+                meet();
+                if (rank)
+                    for (int i = tid; i < kParts; i += kThreads)
+                        if (const uint32_t n = sh.part.count[i]) {
+                            Shared<T> *to = of(0);
+                            atomicAdd(&to->part.count[i], n);
+                            const unsigned long long m = whole(sh.part.mass[i]);
+                            if (m) add_to(&to->part.mass[i], m);
+                        }
+            }
             meet();
-            if (rank == 0) {
-                for (int s = warp; s < kParts / 32; s += kWarps) {
-                    uint32_t count;
-                    unsigned long long mass;
-                    merged(true, s * 32 + lane, base + ((uint32_t)(s * 32 + lane) << shift), shift == 0, count, mass);
-                    count = __reduce_add_sync(0xffffffffu, count);
-                    mass = __shfl_sync(0xffffffffu, scan_sum(mass, lane), 31);
-                    if (lane == 0) { sh.part_step_count[s] = count; sh.part_step_mass[s] = mass; }
+            if (rank == 0) { sum_parts(base, shift); __syncthreads(); }
+        }
+    }
+    // The same among the tokens of bin p.bin, of which there are few: CTA 0 gets a list of them
+    __device__ Place ranked(Mode mode, unsigned long long y, const Place &p) {
+        Shared<T> *to = of(0);
+        mine([&](int i, uint32_t h) {
+            const uint32_t d = K::key(h);
+            if (d == kNone || K::bin(d) != p.bin) return;
+            const uint32_t at = atomicAdd(&to->found, 1u);
+            if (at < kParts) { to->list.key[at] = d; to->list.id[at] = (uint32_t)i; }        // (it is: they have been counted)
+        });
+        meet();
+        if (rank == 0) {
+            const uint32_t n = min(sh.found, (uint32_t)kParts);
+            for (uint32_t j = tid; j < n; j += kThreads) sh.list.w[j] = weight(sh.list.key[j]);
+            __syncthreads();
+            // (up to n: BY_KEY asks for a place behind a key that may have no token)
+            for (uint32_t j = tid; j < n + (mode == BY_KEY); j += kThreads) {
+                if (mode == BY_KEY && j < n) continue;
+                const uint32_t d = j < n ? sh.list.key[j] : (uint32_t)y, id = j < n ? sh.list.id[j] : kNone;
+                uint32_t before = 0, tie = 0;
+                unsigned long long mass = 0;
+#pragma unroll 4
+                for (uint32_t k = 0; k < n; ++k) {
+                    const uint32_t x = sh.list.key[k];
+                    const bool lower = x < d, same = x == d && sh.list.id[k] < id;
+                    before += lower;
+                    tie += same;
+                    if (lower) mass += sh.list.w[k];
                 }
-                __syncthreads();
-                if (warp == 0) run_steps(sh.part_step_count, sh.part_step_mass, kParts / 32);
+                Place q = p;
+                q.d = d; q.tie = tie; q.id = id;
+                q.w = j < n ? sh.list.w[j] : weight(d);
+                q.count_before += before;
+                q.mass_before += mass;
+                const unsigned long long c = (unsigned long long)q.count_before + tie, m = q.mass_before + tie * q.w;
+                if (mode == BY_COUNT ? c == y : mode == BY_MASS ? m <= y && y < m + q.w : true)
+                    for (int r = 0; r < C; ++r) of(r)->place = q;
             }
         }
+        meet();
+        const Place q = sh.place;
+        meet();
+        return q;
     }
 
     // the largest key whose share is at least `least` (0 < least <= 1; the share falls as the key rises)
     __device__ uint32_t last_key(double least) const {
         unsigned long long lo = top, hi = sizeof(T) == 2 ? 0xffffu : 0xffffffffu;       // lo qualifies; hi does not (a NaN's place)
+#pragma unroll 1
         while (hi - lo > 1) {
             const unsigned long long step = (hi - lo + 32) / 33, d = lo + step * (lane + 1);
             const unsigned m = __ballot_sync(0xffffffffu, d < hi && share((uint32_t)d) >= least);
@@ -352,56 +473,87 @@ struct Sampler {
         return (uint32_t)lo;
     }
 
-    // id of the owner_tie-th token with key d among this CTA's; all threads call it
+    // Id of the tie-th token with key d, by the CTA that has it: a bit map of them, a stretch of elements at a time
     __device__ void find_token(const Place &p, int32_t *out) {
-        const int per = (v1 - v0 + kWarps - 1) / kWarps, b = v0 + warp * per, e = min(v1, b + per);
-        uint32_t n = 0;
-        elements(b, e, lane, 32, [&](int, uint32_t h) { n += K::key(h) == p.d; });
-        n = __reduce_add_sync(0xffffffffu, n);
-        if (lane == 0) sh.per_warp[warp] = n;
-        __syncthreads();
-        uint32_t before = 0;
-        for (int k = 0; k < warp; ++k) before += sh.per_warp[k];
-        if (p.owner_tie < before || p.owner_tie >= before + n) return;
-        uint32_t left = p.owner_tie - before;
-        // vectors in order, a lane each
-        for (int v = b; v < e; v += 32) {
-            uint32_t c = 0;
-            if (v + lane < e) elements(v + lane, v + lane + 1, 0, 1, [&](int, uint32_t h) { c += K::key(h) == p.d; });
-            const uint32_t upto = (uint32_t)scan_sum(c, lane);
-            const uint32_t all = __shfl_sync(0xffffffffu, upto, 31);
-            if (left < all) {
-                if (left >= upto - c && left < upto) {
-                    uint32_t k = left - (upto - c);
-                    elements(v + lane, v + lane + 1, 0, 1, [&](int i, uint32_t h) { if (K::key(h) == p.d && k-- == 0) *out = i; });
-                }
-                return;
+        // a stretch per CTA at a time (so that half of a row is read on average); the bits are where the counts were
+        const int room = min(32768, ((a.vocab + C - 1) / C + 31) & ~31);
+        static_assert(32768 <= K::STEPS * 32 * 32, "bit map");
+        // (both zeros are one key)
+        const uint32_t bits = K::bits(p.d) * (K::HALF ? 0x10001u : 1u), mask = K::bits(p.d) ? 0xffffffffu : (K::SIGN - 1) * (K::HALF ? 0x10001u : 1u);
+        uint32_t before = 0;                               // those of earlier stretches
+#pragma unroll 1
+        for (int b = rank; ; b += C) {                     // (every CTA as often: they tell one another how many there are)
+            const int lo = (int)min((long long)a.vocab, (long long)b * room), hi = min(a.vocab, lo + room);
+            __syncthreads();
+            for (int i = tid; i < room / 32; i += kThreads) sh.count[i] = 0;
+            __syncthreads();
+            auto put = [&](int i) { atomicOr(&sh.count[(i - lo) >> 5], 1u << ((i - lo) & 31)); };
+            vectors<4>(lo, hi,
+                    [&](int i0, const uint4 &u) {
+                        uint32_t w[4] = {(u.x ^ bits) & mask, (u.y ^ bits) & mask, (u.z ^ bits) & mask, (u.w ^ bits) & mask};
+                        if constexpr (K::HALF) {
+                            uint32_t eq = 0;               // (a bit an element)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) { const uint32_t e = __vseteq2(w[q], 0); eq |= ((e | e >> 15) & 3) << (2 * q); }
+                            while (eq) { put(i0 + __ffs(eq) - 1); eq &= eq - 1; }
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) if (w[q] == 0) put(i0 + q);
+                        }
+                    },
+                    [&](int i, uint32_t h) { if (K::key(h) == p.d) put(i); });
+            __syncthreads();
+            // how many: of a thread's words, of the threads in front of it, of the CTAs in front of this one
+            const int words = (hi - lo + 31) / 32, per = (words + kThreads - 1) / kThreads, w0 = min(words, tid * per), w1 = min(words, w0 + per);
+            uint32_t n = 0;
+            for (int i = w0; i < w1; ++i) n += __popc(sh.count[i]);
+            const uint32_t upto = scan_sum(n, lane);
+            if (lane == 31) sh.per_warp[warp] = upto;
+            __syncthreads();
+            uint32_t mine = 0, all = 0;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) { if (k < warp) mine += sh.per_warp[k]; all += sh.per_warp[k]; }
+            if (C > 1) {
+                if (tid == 0) sh.found = all;
+                meet();
+                const uint32_t others = lane < C ? of(lane)->found : 0, sum = scan_sum(others, lane);
+                mine += __shfl_sync(0xffffffffu, sum - others, rank);
+                all = __shfl_sync(0xffffffffu, sum, 31);
+                meet();
             }
-            left -= all;
+            uint32_t left = p.tie - before - mine - (upto - n);        // (huge, if it is in front)
+            if (p.tie >= before && left < n)
+                for (int i = w0; ; ++i) {
+                    const uint32_t w = sh.count[i], c = __popc(w);
+                    if (left < c) { *out = lo + i * 32 + (int)__fns(w, 0, (int)left + 1); break; }
+                    left -= c;
+                }
+            before += all;
+            if (p.tie < before || (long long)(b - rank + C) * room >= a.vocab) return;
         }
     }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_tokens_kernel(const SampleArgs a)
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4 : 3) : 1) sample_tokens_kernel(const SampleArgs a)
 {
     using K = Keys<T>;
     extern __shared__ __align__(16) unsigned char smem[];
     Shared<T> &sh = *reinterpret_cast<Shared<T> *>(smem);
     const int tid = threadIdx.x;
-    Sampler<T> s{sh, a, cg::this_cluster()};
+    Sampler<T, kThreads> s{sh, a, cg::this_cluster()};
     s.C = gridDim.x; s.rank = blockIdx.x;
     s.tid = tid; s.lane = tid & 31; s.warp = tid >> 5;
     const int r = blockIdx.y;
     for (int i = tid; i < K::STEPS * 32; i += kThreads) sh.count[i] = 0;
     for (int i = tid; i < K::WEIGHED; i += kThreads) sh.mass[i] = Sum{0, 0};
+    if (tid == 0) sh.top = kNone;
+    if (tid < 32) sh.two_to[tid] = kTwoTo[tid];
     pdl_begin();
     s.row = static_cast<const T *>(a.logits) + r * a.stride;
-    s.skew = (int)((reinterpret_cast<uintptr_t>(s.row) & 15) / sizeof(T));
-    s.n_vec = (a.vocab + s.skew + K::N - 1) / K::N;
-    const int per = (s.n_vec + s.C - 1) / s.C;
-    s.v0 = min(s.n_vec, s.rank * per);
-    s.v1 = min(s.n_vec, s.v0 + per);
+    const int per = (a.vocab + s.C - 1) / s.C;
+    s.e0 = min(a.vocab, s.rank * per);
+    s.e1 = min(a.vocab, s.e0 + per);
     const float t = a.temperature[r];
     const bool greedy = !(t > 0.f);
     s.inv_t = 1.0 / (greedy ? 1.0 : (double)t);
@@ -411,44 +563,77 @@ __global__ void __launch_bounds__(kThreads, 2) sample_tokens_kernel(const Sample
     const double u = fmin(fmax((double)a.u[r], 0.0), 1.0 - 0x1p-24);          // (NaN: 0)
     __syncthreads();
 
-    if constexpr (sizeof(T) == 2) {
-        s.mine([&](int, uint32_t h) {
-            const int b = K::bin_of(h);
-            if (b >= 0) atomicAdd(&sh.count[b], 1u);
-        });
+    auto weigh = [&] { s.x_top = s.top == kNone ? 0.0 : K::value(s.top); };
+    if constexpr (K::HALF) {
+        if (tid == 0) sh.found = 0;
+        __syncthreads();
+        // zero, and what has no bin of its own (whose weights are needed one by one: a list of them); hardly ever
+        auto rare = [&](uint32_t h) {
+            const uint32_t d = K::key(h);
+            if (d == kNone) return;
+            const int b = K::bin(d);
+            atomicAdd(&sh.count[b], 1u);
+            if (b == K::ZERO) return;
+            const uint32_t at = atomicAdd(&sh.found, 1u);
+            if (at < 4 * kParts) sh.wide_bits[at] = h;
+        };
+        uint32_t odd = 0;                                  // a vector's elements that are rare, a bit each
+        auto add = [&](uint32_t h, int k) {
+            const uint32_t t = (h & 0x7fff) - K::LO;
+            if (t < (uint32_t)K::FINE) atomicAdd(&sh.count[h & 0x8000 ? K::FINE + 4 + t : K::FINE - t], 1u);
+            else odd |= 1u << k;
+        };
+        s.template vectors<4>(s.e0, s.e1,
+                  [&](int i0, const uint4 &u) {
+                      odd = 0;
+                      add(u.x & 0xffff, 0); add(u.x >> 16, 1); add(u.y & 0xffff, 2); add(u.y >> 16, 3);
+                      add(u.z & 0xffff, 4); add(u.z >> 16, 5); add(u.w & 0xffff, 6); add(u.w >> 16, 7);
+#pragma unroll 1
+                      while (odd) {
+                          rare((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(s.row) + i0 + __ffs(odd) - 1));
+                          odd &= odd - 1;
+                      }
+                  },
+                  [&](int, uint32_t h) { odd = 0; add(h, 0); if (odd) rare(h); });
+        __syncthreads();
+        const uint32_t listed = sh.found;
+        // the largest: the first bin that is not empty, if that is one value, else by another look at the elements
+        __syncthreads();
+        if (tid == 0) sh.found = K::BINS;
+        __syncthreads();
+        uint32_t first = K::BINS;
+#pragma unroll 1
+        for (int b = tid; b < K::BINS && first == K::BINS; b += kThreads)
+            if (sh.count[b]) first = b;
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (s.lane == 0) atomicMin(&sh.found, first);
+        __syncthreads();
+        first = sh.found;
+        if (first < K::BINS && K::wide(first)) s.find_top();
+        else if (tid == 0 && first < K::BINS) sh.top = K::first(first);
         s.meet();
-        // the largest: the first bin that is not empty; in the bins of many values (and for their weights) by another look at the elements
-        bool many = false;
-        for (int k = 0; k < K::WEIGHED; ++k)
-            for (int q = 0; q < s.C; ++q) many |= s.of(q)->count[k == 0 ? 0 : k == 1 ? K::FINE + 1 : k == 2 ? K::FINE + 3 : K::BINS - 1] != 0;
-        if (many) {
-            s.find_top();
-        } else {
-            if (tid == 0) sh.top = kNone;
-            __syncthreads();
-            for (int b = tid; b < K::BINS; b += kThreads)
-                if (sh.count[b]) { atomicMin(&sh.top, K::first(b)); break; }
-            s.meet();
-            s.top = sh.top;
-            for (int q = 0; q < s.C; ++q) s.top = min(s.top, s.of(q)->top);
-        }
-        s.x_top = s.top == kNone ? 0.0 : K::value(s.top);
-        if (many)
-            s.mine([&](int, uint32_t h) {
-                const int b = K::bin_of(h), m = b < 0 ? -1 : K::weighed(b);
-                if (m >= 0) add_to(&sh.mass[m], s.weight(K::key(h)));
-            });
+        s.top = s.top_of_all();
+        weigh();
+        auto weigh_one = [&](uint32_t h) {
+            const uint32_t d = K::key(h);
+            if (d != kNone && K::wide(K::bin(d))) add_to(&sh.mass[K::weighed(K::bin(d))], s.weight(d));
+        };
+        if (listed <= 4 * kParts) for (uint32_t j = tid; j < listed; j += kThreads) weigh_one(sh.wide_bits[j]);
+        else s.mine([&](int, uint32_t h) { weigh_one(h); });
     } else {
         s.find_top();
-        s.x_top = s.top == kNone ? 0.0 : K::value(s.top);
-        s.mine([&](int, uint32_t h) {
+        s.meet();
+        s.top = s.top_of_all();
+        weigh();
+        const auto add = [&](uint32_t h) {
             const uint32_t d = K::key(h);
             if (d == kNone) return;
             const int b = K::bin(d);
             atomicAdd(&sh.count[b], 1u);
             const unsigned long long w = s.weight(d);
             if (w) add_to(&sh.mass[b], w);
-        });
+        };
+        s.template vectors<2>(s.e0, s.e1, [&](int, const uint4 &u) { add(u.x); add(u.y); add(u.z); add(u.w); }, [&](int, uint32_t h) { add(h); });
     }
     if (s.top == kNone) {
         if (s.rank == 0 && tid == 0) { a.token[r] = 0; if (a.logprob) a.logprob[r] = NAN; }
@@ -458,62 +643,59 @@ __global__ void __launch_bounds__(kThreads, 2) sample_tokens_kernel(const Sample
     s.meet();
     s.sum_steps();
     s.meet();
-    if (s.rank == 0) {
-        if (s.warp == 0) s.run_steps(sh.step_count, sh.step_mass, K::STEPS);
-        __syncthreads();
-    }
-    if (s.C > 1) {
-        // (the others need the totals)
-        if (s.rank == 0 && s.warp == 0 && s.lane < s.C && s.lane) {
+    if (s.rank == 0 && s.warp == 0) {
+        s.run_steps(false);
+        if (s.lane > 0 && s.lane < s.C) {                 // (the others need the totals)
             s.of(s.lane)->step_count[K::STEPS] = sh.step_count[K::STEPS];
             s.of(s.lane)->step_mass[K::STEPS] = sh.step_mass[K::STEPS];
         }
-        s.meet();
     }
+    s.meet();
     const uint32_t tokens = sh.step_count[K::STEPS];
     unsigned long long mass = sh.step_mass[K::STEPS];
-    Place cut;
-    cut.d = kNone; cut.tie = 0;                       // the last token that is kept: (d, tie)
-    bool is_cut = false;
-    if (top_k > 0 && (uint32_t)top_k < tokens) {
-        cut = s.locate(BY_COUNT, (unsigned long long)top_k - 1);
-        mass = cut.mass_before + (cut.tie + 1ull) * cut.w;
-        is_cut = true;
-    }
-    if (top_p < 1.f) {
-        const double want = ceil((double)fmaxf(top_p, 0.f) * (double)mass);
-        const unsigned long long y = want < 1.0 ? 0 : (unsigned long long)want - 1;
-        cut = s.locate(BY_MASS, y);
-        mass = cut.mass_before + (cut.tie + 1ull) * cut.w;
-        is_cut = true;
-    }
-    if (min_p > 0.f) {
-        if (min_p > 1.f) {
-            mass = (unsigned long long)s.scale;       // the first token alone
-        } else {
+    Place at;                                         // the last token that is kept, then the drawn one
+    uint32_t cut = kNone;                             // key of the former
+#pragma unroll 1
+    for (int stage = 0; stage < 4; ++stage) {         // top-k, top-p, min-p, the draw
+        Mode mode = BY_MASS;
+        unsigned long long y;
+        if (stage == 0) {
+            if (top_k <= 0 || (uint32_t)top_k >= tokens) continue;
+            mode = BY_COUNT;
+            y = (unsigned long long)top_k - 1;
+        } else if (stage == 1) {
+            if (!(top_p < 1.f)) continue;
+            const double want = ceil((double)fmaxf(top_p, 0.f) * (double)mass);
+            y = want < 1.0 ? 0 : (unsigned long long)want - 1;
+        } else if (stage == 2) {
+            if (!(min_p > 0.f)) continue;
+            if (min_p > 1.f) { mass = (unsigned long long)s.scale; continue; }        // the first token alone
             const uint32_t d = s.last_key((double)min_p);
-            if (!is_cut || d < cut.d) {
-                const Place q = s.locate(BY_KEY, d);
-                mass = q.mass_before + (unsigned long long)q.tie * q.w;
-            }
+            if (d >= cut) continue;
+            mode = BY_KEY;
+            y = d;
+        } else {
+            y = (unsigned long long)floor(u * (double)mass);
         }
+        at = s.locate(mode, y);
+        if (stage == 3) break;
+        mass = at.mass_before + ((unsigned long long)at.tie + (mode == BY_KEY ? 0 : 1)) * at.w;
+        cut = at.d;
     }
-    const Place drawn = s.locate(BY_MASS, (unsigned long long)floor(u * (double)mass));
-    if (s.rank == (int)drawn.owner) s.find_token(drawn, a.token + r);
+    const Place drawn = at;
+    if (drawn.id == kNone) s.find_token(drawn, a.token + r);
+    else if (s.rank == 0 && tid == 0) a.token[r] = (int32_t)drawn.id;
     if (s.rank == 0 && tid == 0 && a.logprob)
         a.logprob[r] = (float)((drawn.d == s.top ? 0.0 : (K::value(drawn.d) - s.x_top) * s.inv_t) - log((double)mass / s.scale));
 }
 
-template <typename T>
-cudaError_t launch_one(const SampleArgs &a, int rows, cudaStream_t st)
+template <typename T, int kThreads>
+cudaError_t launch_one(const SampleArgs &a, int rows, int C, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = configure(sample_tokens_kernel<T>, done, (int)sizeof(Shared<T>), true);
+    const size_t smem = C > 1 ? sizeof(Shared<T>) : offsetof(Shared<T>, all_count);
+    const cudaError_t e = configure(sample_tokens_kernel<T, kThreads>, done, (int)smem, false);
     if (e != cudaSuccess) return e;
-    // CTAs per row: while they find SMs and have something to count
-    int C = 1;
-    while (C < 16 && (long long)rows * C * 2 <= 2LL * num_sms() && a.vocab / (C * 2) >= 2048) C *= 2;
-    if (C == 16 && clusters_resident(16, 2) < 1) C = 8;
     for (int r0 = 0; r0 < rows; r0 += 65535) {               // (what a grid's second dimension holds)
         const int n = rows - r0 < 65535 ? rows - r0 : 65535;
         SampleArgs b = a;
@@ -523,10 +705,18 @@ cudaError_t launch_one(const SampleArgs &a, int rows, cudaStream_t st)
         if (b.top_p) b.top_p += r0;
         if (b.min_p) b.min_p += r0;
         if (b.logprob) b.logprob += r0;
-        const cudaError_t x = launch_clusters(true, C, sample_tokens_kernel<T>, dim3(C, n), kThreads, sizeof(Shared<T>), st, b);
+        const cudaError_t x = launch_clusters(true, C, sample_tokens_kernel<T, kThreads>, dim3(C, n), kThreads, smem, st, b);
         if (x != cudaSuccess) return x;
     }
     return cudaSuccess;
+}
+
+// CTAs per row: several while they find SMs of their own and have something to count
+template <typename T> cudaError_t launch_type(const SampleArgs &a, int rows, cudaStream_t st)
+{
+    int C = 1;
+    while (C < 8 && (long long)rows * C * 2 <= num_sms() && a.vocab / (C * 2) >= 2048) C *= 2;
+    return C > 1 ? launch_one<T, 512>(a, rows, C, st) : launch_one<T, 256>(a, rows, C, st);
 }
 
 }  // namespace
@@ -540,7 +730,7 @@ cudaError_t launch_sample_tokens(const void *logits, int dtype, int rows, int vo
     a.scale_bits = 62;
     while ((1ll << (62 - a.scale_bits)) < vocab) --a.scale_bits;       // 2^scale_bits * vocab <= 2^62
     a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u; a.token = token; a.logprob = logprob;
-    return dtype == ORTHRUS_FP32 ? launch_one<float>(a, rows, st) : launch_one<__nv_bfloat16>(a, rows, st);
+    return dtype == ORTHRUS_FP32 ? launch_type<float>(a, rows, st) : launch_type<__nv_bfloat16>(a, rows, st);
 }
 
 }  // namespace orthrus
