@@ -36,7 +36,10 @@ template <typename T> struct Keys {
     static constexpr bool HALF = sizeof(T) == 2;
     static constexpr int N = 16 / sizeof(T);                           // elements of 16 bytes
     static constexpr uint32_t LO = (HALF ? 103u : 119u) << 7, HI = 135u << 7;      // magnitudes 2^-24 or 2^-8, and 2^8
-    static constexpr int FINE = HI - LO, BINS = 2 * FINE + 5, STEPS = (BINS + 31) / 32, WEIGHED = HALF ? 4 : BINS;
+    // Groups of 32 bins in the order of values: above, the positive ones, near zero (positive, zero, negative), the negative ones, below
+    static constexpr int FINE = HI - LO, POS = 32, NEAR = POS + FINE, ZERO = NEAR + 1, NEG = NEAR + 32, END = NEG + FINE, STEPS = END / 32 + 1;
+    static constexpr int SLOTS = 2 * FINE + 5, WEIGHED = HALF ? 4 : SLOTS;
+    static_assert(FINE % 32 == 0, "whole groups");
     static constexpr int LOW = HALF ? 0 : 16;                          // bits behind the leading 16
     static constexpr uint32_t SIGN = HALF ? 0x8000u : 0x80000000u, INF = 0x7f80u << LOW;
     using Raw = std::conditional_t<HALF, uint16_t, uint32_t>;
@@ -48,25 +51,33 @@ template <typename T> struct Keys {
     __device__ static uint32_t bits(uint32_t d) { return d < SIGN ? SIGN - 1 - d : d; }
     __device__ static double value(uint32_t d) { return (double)__uint_as_float(bits(d) << (16 - LOW)); }
     __device__ static int bin(uint32_t d) {
-        if (d == SIGN - 1) return FINE + 2;
-        const uint32_t mag = (d < SIGN ? SIGN - 1 - d : d - SIGN) >> LOW;
-        const int t = (int)(min(max(mag, LO - 1), HI) - (LO - 1));
-        return d < SIGN ? FINE + 1 - t : FINE + 3 + t;
+        if (d == SIGN - 1) return ZERO;
+        const bool pos = d < SIGN;
+        const uint32_t mag = (pos ? SIGN - 1 - d : d - SIGN) >> LOW;
+        if (mag - LO < (uint32_t)FINE) return pos ? POS + (int)(HI - 1 - mag) : NEG + (int)(mag - LO);
+        return mag < LO ? (pos ? NEAR : NEAR + 2) : pos ? 0 : END;
     }
-    static constexpr int ZERO = FINE + 2;
-    __device__ static bool wide(int b) { return b == 0 || b == FINE + 1 || b == FINE + 3 || b == BINS - 1; }
-    __device__ static bool one_value(int b) { return HALF && !wide(b); }
-    __device__ static int weighed(int b) { return HALF ? (b == 0 ? 0 : b == FINE + 1 ? 1 : b == FINE + 3 ? 2 : 3) : b; }      // where its mass is
+    __device__ static bool fine(int b) { return (b >= POS && b < NEAR) || (b >= NEG && b < END); }
+    __device__ static bool exists(int b) { return fine(b) || b == 0 || (b >= NEAR && b < NEAR + 3) || b == END; }
+    __device__ static bool wide(int b) { return exists(b) && !fine(b) && b != ZERO; }
+    __device__ static bool one_value(int b) { return HALF && (fine(b) || b == ZERO); }
+    // where the count of a bin that exists is: by magnitude, the positive ones, the negative ones, the other five
+    __device__ static int slot(int b) {
+        if (b >= POS && b < NEAR) return NEAR - 1 - b;
+        if (b >= NEG && b < END) return FINE + (b - NEG);
+        return 2 * FINE + (b == 0 ? 0 : b == END ? 4 : b - NEAR + 1);
+    }
+    __device__ static int weighed(int b) { return HALF ? (b == 0 ? 0 : b == NEAR ? 1 : b == NEAR + 2 ? 2 : 3) : slot(b); }      // its mass
     // log2 of how many keys a bin has at most, and the first
     __device__ static int width(int b) { return wide(b) ? HALF ? 15 : 30 : LOW; }
     __device__ static uint32_t first(int b) {
         const uint32_t more = (1u << LOW) - 1;
+        if (b >= POS && b < NEAR) return SIGN - 1 - ((HI - 1 - (b - POS)) << LOW | more);
+        if (b >= NEG && b < END) return SIGN + ((LO + (uint32_t)(b - NEG)) << LOW);
         if (b == 0) return 0;
-        if (b <= FINE) return SIGN - 1 - ((HI - b) << LOW | more);
-        if (b == FINE + 1) return SIGN - 1 - (((LO - 1) << LOW) | more);
+        if (b == NEAR) return SIGN - 1 - (((LO - 1) << LOW) | more);
         if (b == ZERO) return SIGN - 1;
-        if (b == FINE + 3) return SIGN + 1;
-        return SIGN + ((LO + (uint32_t)(b - FINE - 4)) << LOW);
+        return b == END ? SIGN + (HI << LOW) : SIGN + 1;
     }
 };
 
@@ -118,7 +129,7 @@ struct Place { uint32_t d, tie, count_before, count_at, id; int bin; unsigned lo
 
 constexpr int kPartSteps = kParts / 32;
 template <typename T> struct Shared {
-    uint32_t count[Keys<T>::STEPS * 32];                 // (in the end: the bit map)
+    uint32_t count[Keys<T>::SLOTS + 3];                  // of a bin at its slot (in the end: the bit map)
     Sum mass[Keys<T>::WEIGHED];
     union {
         struct { uint32_t count[kParts]; Sum mass[kParts]; } part;
@@ -128,7 +139,7 @@ template <typename T> struct Shared {
     // CTA 0: sums of the groups of 32 bins, then of all before; behind them those of the parts
     unsigned long long step_mass[Keys<T>::STEPS + 1 + kPartSteps + 1];
     uint32_t step_count[Keys<T>::STEPS + 1 + kPartSteps + 1];
-    Place place;
+    Place place[2];
     uint32_t top, found, per_warp[16];
     double two_to[32];                                   // 2^(j / 32)
     // CTA 0 of several: what all of them have counted (a launch of single CTAs leaves out the room for these)
@@ -174,6 +185,7 @@ struct Sampler {
     int e0, e1;                            // this CTA's elements
     uint32_t top;                          // key of the largest
     double x_top, inv_t, scale;
+    int turn;                              // which of the two places is next (one is written while the other may still be read)
 
     __device__ void meet() { if (C > 1) cluster.sync(); else __syncthreads(); }
     __device__ Shared<T> *of(int r) { return C > 1 ? cluster.map_shared_rank(&sh, r) : &sh; }
@@ -232,64 +244,52 @@ struct Sampler {
 
     // what is in bin b, of parts if `parts`, by its first value d (`one`: it has no other)
     __device__ void in_bin(bool parts, int b, uint32_t d, bool one, uint32_t &count, unsigned long long &mass) {
-        count = parts ? sh.part.count[b] : C > 1 ? sh.all_count[b] : sh.count[b];
+        count = parts ? sh.part.count[b] : C > 1 ? sh.all_count[b] : sh.count[K::slot(b)];
         mass = 0;
         if (one) { if (count) mass = count * weight(d); }
         else mass = whole(parts ? sh.part.mass[b] : C > 1 ? sh.all_mass[K::weighed(b)] : sh.mass[K::weighed(b)]);
     }
-    // Sums of groups of 32 bins to CTA 0, and, where there are several CTAs, of the bins themselves; groups shared out over warps and CTAs, two
-    // at a time, whose exponentials run side by side.
+    // Sums of groups of 32 bins to CTA 0, and, where there are several CTAs, of the bins themselves; groups shared out over warps and CTAs.
+    // (A loop of few instructions: these are what many rows wait for.)
     __device__ void sum_steps() {
         Shared<T> *to = of(0);
-        constexpr int U = 2;
 #pragma unroll 1
-        for (int s0 = rank * kWarps + warp; s0 < K::STEPS; s0 += U * C * kWarps) {
-            uint32_t count[U];
-            unsigned long long mass[U];
-            bool one[U], wide[U];
-            int b[U];
+        for (int s = rank * kWarps + warp; s < K::STEPS; s += C * kWarps) {
+            const int b = s * 32 + lane;
+            // slot, and, of a fine bin of bf16, the value; groups are of one kind
+            const bool pos = s >= K::POS / 32 && s < K::NEAR / 32, neg = s >= K::NEG / 32 && s < K::END / 32, is = pos || neg || K::exists(b);
+            const int at = pos ? K::NEAR - 1 - b : neg ? K::FINE + (b - K::NEG) : is ? K::slot(b) : 0;
+            const bool one = is && (pos || neg ? K::HALF : K::one_value(b)), wide = is && !one;
+            uint32_t count = 0;
+            unsigned long long mass = 0;
+            if (C == 1) {
+                if (is) count = sh.count[at];
+                if (wide) mass = whole(sh.mass[K::weighed(b)]);
+            } else {
+                const Sum *m = sh.mass + (wide ? K::weighed(b) : 0);
+                uint32_t x[8];
+                Sum y[8];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int s = s0 + k * C * kWarps;
-                b[k] = min(s * 32 + lane, K::STEPS * 32 - 1);
-                const bool is = s < K::STEPS && b[k] < K::BINS;
-                one[k] = is && K::one_value(b[k]);
-                wide[k] = is && !one[k];
-                count[k] = 0;
-                mass[k] = 0;
-                if (C == 1) {
-                    if (is) count[k] = sh.count[b[k]];
-                    if (wide[k]) mass[k] = whole(sh.mass[K::weighed(b[k])]);
-                } else {
-                    const Sum *m = sh.mass + (wide[k] ? K::weighed(b[k]) : 0);
-                    uint32_t x[8];
-                    Sum y[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {              // (at most eight CTAs)
-                        x[i] = is && i < C ? *cluster.map_shared_rank(sh.count + b[k], i) : 0;
-                        y[i] = wide[k] && i < C ? *cluster.map_shared_rank(m, i) : Sum{0, 0};
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { count[k] += x[i]; mass[k] += whole(y[i]); }
-                    if (is) to->all_count[b[k]] = count[k];
-                    if (wide[k]) to->all_mass[K::weighed(b[k])] = Sum{(uint32_t)mass[k], (uint32_t)(mass[k] >> 32)};
+                for (int i = 0; i < 8; ++i) {              // (at most eight CTAs)
+                    x[i] = is && i < C ? *cluster.map_shared_rank(sh.count + at, i) : 0;
+                    y[i] = wide && i < C ? *cluster.map_shared_rank(m, i) : Sum{0, 0};
                 }
-            }
-            if (K::HALF && __any_sync(0xffffffffu, count[0] | count[U - 1])) {
-                unsigned long long w[U];
 #pragma unroll
-                for (int k = 0; k < U; ++k) w[k] = weight(K::first(min(b[k], K::BINS - 1)));
-#pragma unroll
-                for (int k = 0; k < U; ++k) if (one[k]) mass[k] = count[k] * w[k];
+                for (int i = 0; i < 8; ++i) { count += x[i]; mass += whole(y[i]); }
+                to->all_count[b] = count;
+                if (wide) to->all_mass[K::weighed(b)] = Sum{(uint32_t)mass, (uint32_t)(mass >> 32)};
             }
-#pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int s = s0 + k * C * kWarps;
-                const uint32_t n = __reduce_add_sync(0xffffffffu, count[k]);
-                unsigned long long m = 0;
-                if (n) m = warp_total(mass[k]);
-                if (lane == 0 && s < K::STEPS) { to->step_count[s] = n; to->step_mass[s] = m; }
+            uint32_t n = 0;
+            if (__any_sync(0xffffffffu, count)) {
+                if (one) {
+                    const uint32_t h = pos ? K::LO + at : neg ? 0x8000u + K::LO + (at - K::FINE) : K::bits(K::first(b));
+                    const double y = ((double)__uint_as_float(h << 16) - x_top) * inv_t;
+                    mass = count * __double2ull_rn((K::bits(top) == h ? 1.0 : exp_of(y, sh.two_to)) * scale);
+                }
+                n = __reduce_add_sync(0xffffffffu, count);
+                mass = warp_total(mass);
             }
+            if (lane == 0) { to->step_count[s] = n; to->step_mass[s] = mass; }
         }
     }
     // the same for the parts, all of which are CTA 0's
@@ -340,10 +340,11 @@ struct Sampler {
             s = min((int)__reduce_add_sync(0xffffffffu, below), n - 1);
         }
         const int b = s * 32 + lane;
-        const uint32_t d = parts ? base + ((uint32_t)b << shift) : b < K::BINS ? K::first(b) : kNone;
+        const bool is = parts || K::exists(b);
+        const uint32_t d = parts ? base + ((uint32_t)b << shift) : is ? K::first(b) : kNone;
         uint32_t count = 0;
         unsigned long long mass = 0;
-        if (parts || b < K::BINS) in_bin(parts, b, d, parts ? shift == 0 : K::one_value(b), count, mass);
+        if (is) in_bin(parts, b, d, parts ? shift == 0 : K::one_value(b), count, mass);
         const uint32_t cb = p.count_before + sc[s] + scan_sum(count, lane) - count;
         const unsigned long long mb = p.mass_before + sm[s] + scan_sum(mass, lane) - mass;
         const unsigned hit = mode == BY_KEY ? 1u << (by_key & 31)
@@ -379,12 +380,13 @@ struct Sampler {
                     else if (mode == BY_MASS) p.tie = p.w ? (uint32_t)min((y - p.mass_before) / p.w, (unsigned long long)p.count_at - 1) : 0;
                     else p.tie = p.count_at;                              // (one behind the last of them)
                 }
-                if (lane < C) of(lane)->place = p;
+                if (lane < C) of(lane)->place[turn] = p;
                 if (lane == 0) sh.found = 0;
             }
             meet();
-            p = sh.place;
-            if (parts ? shift == 0 : K::one_value(p.bin)) { meet(); return p; }
+            p = sh.place[turn];
+            turn ^= 1;
+            if (parts ? shift == 0 : K::one_value(p.bin)) return p;
             if (!parts && p.count_at <= kParts) return ranked(mode, y, p);
             // the bin's parts
             base = p.d;
@@ -450,12 +452,12 @@ struct Sampler {
                 q.mass_before += mass;
                 const unsigned long long c = (unsigned long long)q.count_before + tie, m = q.mass_before + tie * q.w;
                 if (mode == BY_COUNT ? c == y : mode == BY_MASS ? m <= y && y < m + q.w : true)
-                    for (int r = 0; r < C; ++r) of(r)->place = q;
+                    for (int r = 0; r < C; ++r) of(r)->place[turn] = q;
             }
         }
         meet();
-        const Place q = sh.place;
-        meet();
+        const Place q = sh.place[turn];
+        turn ^= 1;
         return q;
     }
 
@@ -477,7 +479,7 @@ struct Sampler {
     __device__ void find_token(const Place &p, int32_t *out) {
         // a stretch per CTA at a time (so that half of a row is read on average); the bits are where the counts were
         const int room = min(32768, ((a.vocab + C - 1) / C + 31) & ~31);
-        static_assert(32768 <= K::STEPS * 32 * 32, "bit map");
+        static_assert(32768 <= K::SLOTS * 32, "bit map");
         // (both zeros are one key)
         const uint32_t bits = K::bits(p.d) * (K::HALF ? 0x10001u : 1u), mask = K::bits(p.d) ? 0xffffffffu : (K::SIGN - 1) * (K::HALF ? 0x10001u : 1u);
         uint32_t before = 0;                               // those of earlier stretches
@@ -542,10 +544,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
     Shared<T> &sh = *reinterpret_cast<Shared<T> *>(smem);
     const int tid = threadIdx.x;
     Sampler<T, kThreads> s{sh, a, cg::this_cluster()};
-    s.C = gridDim.x; s.rank = blockIdx.x;
+    s.C = gridDim.x; s.rank = blockIdx.x; s.turn = 0;
     s.tid = tid; s.lane = tid & 31; s.warp = tid >> 5;
     const int r = blockIdx.y;
-    for (int i = tid; i < K::STEPS * 32; i += kThreads) sh.count[i] = 0;
+    for (int i = tid; i < K::SLOTS; i += kThreads) sh.count[i] = 0;
     for (int i = tid; i < K::WEIGHED; i += kThreads) sh.mass[i] = Sum{0, 0};
     if (tid == 0) sh.top = kNone;
     if (tid < 32) sh.two_to[tid] = kTwoTo[tid];
@@ -568,52 +570,46 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
         if (tid == 0) sh.found = 0;
         __syncthreads();
         // zero, and what has no bin of its own (whose weights are needed one by one: a list of them); hardly ever
+        __nv_bfloat162 high = __halves2bfloat162(__ushort_as_bfloat16(0xff80), __ushort_as_bfloat16(0xff80));     // (NaN is passed over)
+        uint32_t best = kNone;
         auto rare = [&](uint32_t h) {
             const uint32_t d = K::key(h);
             if (d == kNone) return;
+            best = min(best, d);
             const int b = K::bin(d);
-            atomicAdd(&sh.count[b], 1u);
-            if (b == K::ZERO) return;
+            atomicAdd(&sh.count[K::slot(b)], 1u);
+            if (b == K::ZERO || K::one_value(b)) return;
             const uint32_t at = atomicAdd(&sh.found, 1u);
             if (at < 4 * kParts) sh.wide_bits[at] = h;
         };
-        uint32_t odd = 0;                                  // a vector's elements that are rare, a bit each
-        auto add = [&](uint32_t h, int k) {
-            const uint32_t t = (h & 0x7fff) - K::LO;
-            if (t < (uint32_t)K::FINE) atomicAdd(&sh.count[h & 0x8000 ? K::FINE + 4 + t : K::FINE - t], 1u);
-            else odd |= 1u << k;
+        // a word's two elements, both with bins of their own: the slot is the magnitude's, FINE further on for a negative one
+        char *slots = reinterpret_cast<char *>(sh.count) - 4 * K::LO;
+        auto add = [&](uint32_t w) {
+            constexpr uint32_t BACK = 4 * (0x8000 - K::FINE);
+            atomicAdd(reinterpret_cast<uint32_t *>(slots + ((w << 2 & 0x3fffc) - (w >> 15 & 1) * BACK)), 1u);
+            atomicAdd(reinterpret_cast<uint32_t *>(slots + ((w >> 14 & 0x3fffc) - (w >> 31) * BACK)), 1u);
         };
         s.template vectors<4>(s.e0, s.e1,
                   [&](int i0, const uint4 &u) {
-                      odd = 0;
-                      add(u.x & 0xffff, 0); add(u.x >> 16, 1); add(u.y & 0xffff, 2); add(u.y >> 16, 3);
-                      add(u.z & 0xffff, 4); add(u.z >> 16, 5); add(u.w & 0xffff, 6); add(u.w >> 16, 7);
+                      const uint32_t x = u.x & 0x7fff7fff, y = u.y & 0x7fff7fff, z = u.z & 0x7fff7fff, w = u.w & 0x7fff7fff;
+                      const uint32_t lo = __vminu2(__vminu2(x, y), __vminu2(z, w)), hi = __vmaxu2(__vmaxu2(x, y), __vmaxu2(z, w));
+                      auto pair = [](uint32_t v) { return *reinterpret_cast<__nv_bfloat162 *>(&v); };
+                      high = __hmax2(high, __hmax2(__hmax2(pair(u.x), pair(u.y)), __hmax2(pair(u.z), pair(u.w))));
+                      if (min(lo & 0xffff, lo >> 16) >= K::LO && max(hi & 0xffff, hi >> 16) < K::HI) {
+                          add(u.x); add(u.y); add(u.z); add(u.w);
+                      } else {
 #pragma unroll 1
-                      while (odd) {
-                          rare((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(s.row) + i0 + __ffs(odd) - 1));
-                          odd &= odd - 1;
+                          for (int k = 0; k < K::N; ++k) rare((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(s.row) + i0 + k));
                       }
                   },
-                  [&](int, uint32_t h) { odd = 0; add(h, 0); if (odd) rare(h); });
-        __syncthreads();
-        const uint32_t listed = sh.found;
-        // the largest: the first bin that is not empty, if that is one value, else by another look at the elements
-        __syncthreads();
-        if (tid == 0) sh.found = K::BINS;
-        __syncthreads();
-        uint32_t first = K::BINS;
-#pragma unroll 1
-        for (int b = tid; b < K::BINS && first == K::BINS; b += kThreads)
-            if (sh.count[b]) first = b;
-        first = __reduce_min_sync(0xffffffffu, first);
-        if (s.lane == 0) atomicMin(&sh.found, first);
-        __syncthreads();
-        first = sh.found;
-        if (first < K::BINS && K::wide(first)) s.find_top();
-        else if (tid == 0 && first < K::BINS) sh.top = K::first(first);
+                  [&](int, uint32_t h) { rare(h); });
+        best = min(best, min(K::key(__bfloat16_as_ushort(high.x)), K::key(__bfloat16_as_ushort(high.y))));
+        best = __reduce_min_sync(0xffffffffu, best);
+        if (s.lane == 0) atomicMin(&sh.top, best);
         s.meet();
         s.top = s.top_of_all();
         weigh();
+        const uint32_t listed = sh.found;
         auto weigh_one = [&](uint32_t h) {
             const uint32_t d = K::key(h);
             if (d != kNone && K::wide(K::bin(d))) add_to(&sh.mass[K::weighed(K::bin(d))], s.weight(d));
@@ -629,9 +625,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
             const uint32_t d = K::key(h);
             if (d == kNone) return;
             const int b = K::bin(d);
-            atomicAdd(&sh.count[b], 1u);
+            atomicAdd(&sh.count[K::slot(b)], 1u);
             const unsigned long long w = s.weight(d);
-            if (w) add_to(&sh.mass[b], w);
+            if (w) add_to(&sh.mass[K::weighed(b)], w);
         };
         s.template vectors<2>(s.e0, s.e1, [&](int, const uint4 &u) { add(u.x); add(u.y); add(u.z); add(u.w); }, [&](int, uint32_t h) { add(h); });
     }
