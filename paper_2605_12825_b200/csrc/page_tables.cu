@@ -18,7 +18,7 @@ namespace orthrus {
 namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
-constexpr int kStretch = 256;                    // slots a warp maps at a time
+constexpr int kStretch = 256;                    // slots of a long row that a warp maps at a time
 
 struct Entry { uint32_t gives, takes; int need, held; };       // sums before / up to and with the request; need < 0: left alone
 
@@ -87,51 +87,79 @@ __global__ void __launch_bounds__(kThreads, 1) page_tables_kernel(const PageTabl
     if (flags && lane == 0 && rank == 0 && p.status) atomicOr(p.status, flags);
     __syncthreads();
 
-    // pages that are given back
-    const int first = rank * kWarps + warp, stride = C * kWarps;
-    for (int b = first; b < p.B; b += stride) {
-        const Entry e = entry[b];
-        if (e.need < 0) continue;
-        for (int j = e.need + lane; j < e.held; j += 32) {
-            const unsigned long long at = (unsigned long long)n_free + e.gives + (j - e.need);
-            if (at < (unsigned long long)p.n_pages) p.free_list[at] = p.table[(long long)b * p.max_pages + j];
+    // Page number t of all that are given back, or taken, is a thread's; whose it is, a search in the sums tells.
+    auto request_of = [&](unsigned t, auto upto) {             // the first request that upto(request) is above t for
+        int lo = 0, n = p.B;
+#pragma unroll 1
+        while (n > 1) {
+            const int half = n >> 1;
+            if (upto(lo + half - 1) <= t) { lo += half; n -= half; }
+            else n = half;
         }
+        return lo;
+    };
+    const unsigned mine = rank * kThreads + tid, all = C * kThreads;
+    const unsigned n_given = (unsigned)min(given, (unsigned long long)(p.n_pages - n_free));
+#pragma unroll 1
+    for (unsigned t = mine; t < n_given; t += all) {
+        const int b = request_of(t, [&](int i) { const Entry &e = entry[i]; return e.gives + (e.need >= 0 ? max(e.held - e.need, 0) : 0); });
+        const Entry e = entry[b];
+        p.free_list[n_free + t] = p.table[(long long)b * p.max_pages + e.need + (t - e.gives)];
     }
     cluster_sync_all();
 
-    // pages that are taken
-    auto taken = [&](const Entry &e, int j) {                  // page j >= held of a request that is served
-        return __ldcg(p.free_list + (total - 1 - (e.takes - (unsigned)(e.need - e.held) + (unsigned)(j - e.held))));
-    };
-    for (int b = first; b < p.B; b += stride) {
+    auto taken = [&](unsigned t) { return __ldcg(p.free_list + (total - 1 - t)); };
+#pragma unroll 1
+    for (unsigned t = mine; t < upto; t += all) {
+        const int b = request_of(t, [&](int i) { return entry[i].takes; });
         const Entry e = entry[b];
-        for (int j = e.held + lane; j < e.need; j += 32) p.table[(long long)b * p.max_pages + j] = taken(e, j);
+        p.table[(long long)b * p.max_pages + e.held + (t - (e.takes - (unsigned)(e.need - e.held)))] = taken(t);
     }
-    // slots: a stretch of a request's rows at a time
-    const int stretches = (p.max_new + kStretch - 1) / kStretch;
-    for (long long it = first; it < (long long)p.B * stretches; it += stride) {
-        const int b = (int)(it / stretches), i0 = (int)(it - (long long)b * stretches) * kStretch;
-        const Entry e = entry[b];
-        const int len = p.cache_len[b], n = e.need < 0 ? 0 : p.n_new[b];
-        int64_t *out = p.slot_map + (long long)b * p.max_new;
-        const int32_t *mine = p.table + (long long)b * p.max_pages;
+    // The page of position pos of a request: one that it held, or one that it has just got.  (Both are asked for where they are: the table
+    // of this call's pages may still be on its way.)
+    auto page_of = [&](const Entry &e, const int32_t *held, int pos) {
+        const int j = pos >> p.page_shift;
+        return j < e.held ? held + j : p.free_list + (total - 1 - (e.takes - (unsigned)(e.need - e.held) + (unsigned)(j - e.held)));
+    };
+    const int page_mask = (1 << p.page_shift) - 1;
+    if (p.max_new >= kStretch) {
+        // long rows: a warp 256 slots of a request, eight lookups of a lane under way together
+        const int stretches = (p.max_new + kStretch - 1) / kStretch;
+#pragma unroll 1
+        for (long long it = rank * kWarps + warp; it < (long long)p.B * stretches; it += C * kWarps) {
+            const int b = (int)(it / stretches), i0 = (int)(it - (long long)b * stretches) * kStretch + lane;
+            const Entry e = entry[b];
+            const int len = p.cache_len[b], n = e.need < 0 ? 0 : p.n_new[b];
+            const int32_t *held = p.table + (long long)b * p.max_pages;
+            int64_t *out = p.slot_map + (long long)b * p.max_new;
+            int32_t page[kStretch / 32];
 #pragma unroll
-        for (int k = 0; k < kStretch / 32; ++k) {
-            const int i = i0 + k * 32 + lane;
-            if (i >= p.max_new) break;
-            long long slot = -1;
-            if (i < n) {
-                const int pos = len + i, j = pos >> p.page_shift;
-                const long long page = j < e.held ? mine[j] : taken(e, j);
-                slot = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+            for (int k = 0; k < kStretch / 32; ++k) page[k] = i0 + k * 32 < n ? __ldcg(page_of(e, held, len + i0 + k * 32)) : -1;
+#pragma unroll
+            for (int k = 0; k < kStretch / 32; ++k) {
+                const int i = i0 + k * 32;
+                if (i < p.max_new) out[i] = i < n ? ((long long)page[k] << p.page_shift) + ((len + i) & page_mask) : -1;
             }
-            out[i] = slot;
+        }
+    } else {
+        // short ones: a thread one at a time of all requests' rows laid end to end, so that all threads are busy
+        const long long n_slots = (long long)p.B * p.max_new;
+        const int step_b = (int)(all / (unsigned)p.max_new), step_i = (int)(all % (unsigned)p.max_new);
+        int b = (int)(mine / (unsigned)p.max_new), i = (int)(mine % (unsigned)p.max_new);
+#pragma unroll 4
+        for (long long it = mine; it < n_slots; it += all) {
+            const Entry e = entry[b];
+            const int len = p.cache_len[b], n = e.need < 0 ? 0 : p.n_new[b];
+            p.slot_map[it] = i < n ? ((long long)__ldcg(page_of(e, p.table + (long long)b * p.max_pages, len + i)) << p.page_shift) + ((len + i) & page_mask) : -1;
+            b += step_b;
+            i += step_i;
+            if (i >= p.max_new) { i -= p.max_new; ++b; }
         }
     }
-    for (int b = rank * kThreads + tid; b < p.B; b += C * kThreads) {
-        const Entry e = entry[b];
-        p.granted[b] = e.need < 0 ? 0 : p.n_new[b];
-        p.held_out[b] = e.need < 0 ? e.held : e.need;
+    for (int r = (int)mine; r < p.B; r += (int)all) {
+        const Entry e = entry[r];
+        p.granted[r] = e.need < 0 ? 0 : p.n_new[r];
+        p.held_out[r] = e.need < 0 ? e.held : e.need;
     }
     if (rank == 0 && tid == 0) *p.n_free_out = (int)(total - upto);
 }
@@ -141,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) page_tables_kernel(const PageTabl
 cudaError_t launch_page_tables(const PageTablesParams &p, cudaStream_t st)
 {
     // CTAs by the slots to write
-    const long long slots = (long long)p.B * ((p.max_new + 31) / 32 * 32);
+    const long long slots = (long long)p.B * p.max_new;
     int C = slots <= 8192 ? 1 : slots <= 32768 ? 4 : 8;
     if (slots > 131072 && clusters_resident(16, 1) > 0) C = 16;
     static std::atomic<uint64_t> done{0};
