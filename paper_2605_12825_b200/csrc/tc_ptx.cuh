@@ -160,9 +160,9 @@ __device__ inline uint64_t make_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_
     d |= 2ull << 61;
     return d;
 }
-// instruction descriptor: D fp32, A/B bf16, M = 128, N = n; b_mn = 1 when B is MN-major
-__host__ __device__ constexpr uint32_t make_idesc(uint32_t n, uint32_t b_mn) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+// instruction descriptor: D fp32, A/B bf16, M = m (64: rows 16 w to 16 w + 15 in lanes 32 w to 32 w + 15), N = n; b_mn = 1 when B is MN-major
+__host__ __device__ constexpr uint32_t make_idesc(uint32_t n, uint32_t b_mn, uint32_t m = 128) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 // D[tmem] (+)= A[smem] . B[smem]
 __device__ inline void umma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
