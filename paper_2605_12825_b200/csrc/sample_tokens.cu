@@ -582,21 +582,24 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
             const uint32_t at = atomicAdd(&sh.found, 1u);
             if (at < 4 * kParts) sh.wide_bits[at] = h;
         };
-        // a word's two elements, both with bins of their own: the slot is the magnitude's, FINE further on for a negative one
-        char *slots = reinterpret_cast<char *>(sh.count) - 4 * K::LO;
-        auto add = [&](uint32_t w) {
-            constexpr uint32_t BACK = 4 * (0x8000 - K::FINE);
-            atomicAdd(reinterpret_cast<uint32_t *>(slots + ((w << 2 & 0x3fffc) - (w >> 15 & 1) * BACK)), 1u);
-            atomicAdd(reinterpret_cast<uint32_t *>(slots + ((w >> 14 & 0x3fffc) - (w >> 31) * BACK)), 1u);
+        // Two elements less LO each, both with bins of their own: a magnitude of 12 bits and the sign on top.  The slot is the magnitude's, FINE
+        // further on for a negative one, so the sign moves down to bit 12.  (What a token costs here is instructions.)
+        static_assert(K::FINE == 0x1000, "12 bits");
+        auto add = [&](uint32_t t) {
+            const uint32_t v = (t & 0x0fff0fff) | (t >> 3 & ~0x0fff0fffu);        // (bits 13 to 15 of the lower one are not its own)
+            atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(sh.count) + (v << 2 & 0x7ffc)), 1u);
+            atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(sh.count) + (v >> 14 & ~3u)), 1u);
         };
         s.template vectors<4>(s.e0, s.e1,
                   [&](int i0, const uint4 &u) {
-                      const uint32_t x = u.x & 0x7fff7fff, y = u.y & 0x7fff7fff, z = u.z & 0x7fff7fff, w = u.w & 0x7fff7fff;
-                      const uint32_t lo = __vminu2(__vminu2(x, y), __vminu2(z, w)), hi = __vmaxu2(__vmaxu2(x, y), __vmaxu2(z, w));
+                      // a magnitude below LO or from HI on leaves one of the bits 12 to 14 (a borrow from the upper element does not hide the
+                      // lower one's)
+                      constexpr uint32_t LO2 = K::LO * 0x10001u;
+                      const uint32_t x = u.x - LO2, y = u.y - LO2, z = u.z - LO2, w = u.w - LO2;
                       auto pair = [](uint32_t v) { return *reinterpret_cast<__nv_bfloat162 *>(&v); };
                       high = __hmax2(high, __hmax2(__hmax2(pair(u.x), pair(u.y)), __hmax2(pair(u.z), pair(u.w))));
-                      if (min(lo & 0xffff, lo >> 16) >= K::LO && max(hi & 0xffff, hi >> 16) < K::HI) {
-                          add(u.x); add(u.y); add(u.z); add(u.w);
+                      if (((x | y | z | w) & 0x70007000) == 0) {
+                          add(x); add(y); add(z); add(w);
                       } else {
 #pragma unroll 1
                           for (int k = 0; k < K::N; ++k) rare((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(s.row) + i0 + k));
