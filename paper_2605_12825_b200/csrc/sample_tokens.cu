@@ -68,6 +68,10 @@ template <typename T> struct Keys {
         return 2 * FINE + (b == 0 ? 0 : b == END ? 4 : b - NEAR + 1);
     }
     __device__ static int weighed(int b) { return HALF ? (b == 0 ? 0 : b == NEAR ? 1 : b == NEAR + 2 ? 2 : 3) : slot(b); }      // its mass
+    // the first key behind a bin that exists
+    __device__ static uint32_t end(int b) {
+        return fine(b) ? first(b) + (1u << LOW) : b == 0 ? first(POS) : b == NEAR ? SIGN - 1 : b == ZERO ? SIGN : b == END ? kNone : first(NEG);
+    }
     // log2 of how many keys a bin has at most, and the first
     __device__ static int width(int b) { return wide(b) ? HALF ? 15 : 30 : LOW; }
     __device__ static uint32_t first(int b) {
@@ -177,6 +181,7 @@ template <typename T, int kThreads>
 struct Sampler {
     using K = Keys<T>;
     static constexpr int kWarps = kThreads / 32;
+    static constexpr bool kAlone = kThreads == 256;       // one CTA a row
     Shared<T> &sh;
     const SampleArgs &a;
     cg::cluster_group cluster;
@@ -187,8 +192,8 @@ struct Sampler {
     double x_top, inv_t, scale;
     int turn;                              // which of the two places is next (one is written while the other may still be read)
 
-    __device__ void meet() { if (C > 1) cluster.sync(); else __syncthreads(); }
-    __device__ Shared<T> *of(int r) { return C > 1 ? cluster.map_shared_rank(&sh, r) : &sh; }
+    __device__ void meet() { if (!kAlone) cluster.sync(); else __syncthreads(); }
+    __device__ Shared<T> *of(int r) { return !kAlone ? cluster.map_shared_rank(&sh, r) : &sh; }
     __device__ double share(uint32_t d) const {            // exp((x - max) / T)
         return d == top ? 1.0 : exp_of((K::value(d) - x_top) * inv_t, sh.two_to);
     }
@@ -200,18 +205,14 @@ struct Sampler {
         const int skew = (int)((reinterpret_cast<uintptr_t>(row + b) & 15) / sizeof(T)), head = min((K::N - skew) % K::N, e - b);
         const int n = (e - b - head) / K::N, tail = b + head + n * K::N;
         const uint4 *x = reinterpret_cast<const uint4 *>(row + b + head);
-        int v = tid;
 #pragma unroll 1
-        for (; v + (U - 1) * kThreads < n; v += U * kThreads) {
+        for (int v = tid; v < n; v += U * kThreads) {
             uint4 u[U];
 #pragma unroll
-            for (int q = 0; q < U; ++q) u[q] = __ldg(x + v + q * kThreads);
+            for (int q = 0; q < U; ++q) u[q] = __ldg(x + min(v + q * kThreads, n - 1));
 #pragma unroll
-            for (int q = 0; q < U; ++q) f(b + head + (v + q * kThreads) * K::N, u[q]);
+            for (int q = 0; q < U; ++q) if (v + q * kThreads < n) f(b + head + (v + q * kThreads) * K::N, u[q]);
         }
-        if (U > 1)
-#pragma unroll 1
-            for (; v < n; v += kThreads) f(b + head + v * K::N, __ldg(x + v));
         // (at most N - 1 each, fewer than the threads)
         const int i = tid < head ? b + tid : tid - head < e - tail ? tail + tid - head : -1;
         if (i >= 0) g(i, (uint32_t)__ldg(reinterpret_cast<const typename K::Raw *>(row) + i));
@@ -244,52 +245,68 @@ struct Sampler {
 
     // what is in bin b, of parts if `parts`, by its first value d (`one`: it has no other)
     __device__ void in_bin(bool parts, int b, uint32_t d, bool one, uint32_t &count, unsigned long long &mass) {
-        count = parts ? sh.part.count[b] : C > 1 ? sh.all_count[b] : sh.count[K::slot(b)];
+        count = parts ? sh.part.count[b] : !kAlone ? sh.all_count[b] : sh.count[K::slot(b)];
         mass = 0;
         if (one) { if (count) mass = count * weight(d); }
-        else mass = whole(parts ? sh.part.mass[b] : C > 1 ? sh.all_mass[K::weighed(b)] : sh.mass[K::weighed(b)]);
+        else mass = whole(parts ? sh.part.mass[b] : !kAlone ? sh.all_mass[K::weighed(b)] : sh.mass[K::weighed(b)]);
     }
-    // Sums of groups of 32 bins to CTA 0, and, where there are several CTAs, of the bins themselves; groups shared out over warps and CTAs.
-    // (A loop of few instructions: these are what many rows wait for.)
+    // Sums of groups of 32 bins to CTA 0, and, where there are several CTAs, of the bins themselves; groups shared out over warps and CTAs.  A
+    // warp has J groups under way together, since one's exponentials are a chain that it would wait for.
     __device__ void sum_steps() {
+        constexpr int J = kAlone ? 2 : 1;
         Shared<T> *to = of(0);
 #pragma unroll 1
-        for (int s = rank * kWarps + warp; s < K::STEPS; s += C * kWarps) {
-            const int b = s * 32 + lane;
-            // slot, and, of a fine bin of bf16, the value; groups are of one kind
-            const bool pos = s >= K::POS / 32 && s < K::NEAR / 32, neg = s >= K::NEG / 32 && s < K::END / 32, is = pos || neg || K::exists(b);
-            const int at = pos ? K::NEAR - 1 - b : neg ? K::FINE + (b - K::NEG) : is ? K::slot(b) : 0;
-            const bool one = is && (pos || neg ? K::HALF : K::one_value(b)), wide = is && !one;
-            uint32_t count = 0;
-            unsigned long long mass = 0;
-            if (C == 1) {
-                if (is) count = sh.count[at];
-                if (wide) mass = whole(sh.mass[K::weighed(b)]);
-            } else {
-                const Sum *m = sh.mass + (wide ? K::weighed(b) : 0);
-                uint32_t x[8];
-                Sum y[8];
+        for (int s0 = rank * kWarps + warp; s0 < K::STEPS; s0 += J * C * kWarps) {
+            uint32_t count[J], h[J];
+            unsigned long long mass[J];
+            bool one[J], any = false;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {              // (at most eight CTAs)
-                    x[i] = is && i < C ? *cluster.map_shared_rank(sh.count + at, i) : 0;
-                    y[i] = wide && i < C ? *cluster.map_shared_rank(m, i) : Sum{0, 0};
-                }
+            for (int j = 0; j < J; ++j) {
+                const int s = s0 + j * kWarps, b = s * 32 + lane;
+                // slot, and, of a fine bin of bf16, the value; groups are of one kind
+                const bool pos = s >= K::POS / 32 && s < K::NEAR / 32, neg = s >= K::NEG / 32 && s < K::END / 32;
+                const bool is = pos || neg || (s < K::STEPS && K::exists(b));
+                const int at = pos ? K::NEAR - 1 - b : neg ? K::FINE + (b - K::NEG) : is ? K::slot(b) : 0;
+                one[j] = is && (pos || neg ? K::HALF : K::one_value(b));
+                const bool wide = is && !one[j];
+                h[j] = pos ? K::LO + at : neg ? 0x8000u + K::LO + (at - K::FINE) : is ? K::bits(K::first(b)) : 0;
+                count[j] = 0;
+                mass[j] = 0;
+                if (kAlone) {
+                    if (is) count[j] = sh.count[at];
+                    if (wide) mass[j] = whole(sh.mass[K::weighed(b)]);
+                } else {
+                    const Sum *m = sh.mass + (wide ? K::weighed(b) : 0);
+                    uint32_t x[8];
+                    Sum y[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) { count += x[i]; mass += whole(y[i]); }
-                to->all_count[b] = count;
-                if (wide) to->all_mass[K::weighed(b)] = Sum{(uint32_t)mass, (uint32_t)(mass >> 32)};
-            }
-            uint32_t n = 0;
-            if (__any_sync(0xffffffffu, count)) {
-                if (one) {
-                    const uint32_t h = pos ? K::LO + at : neg ? 0x8000u + K::LO + (at - K::FINE) : K::bits(K::first(b));
-                    const double y = ((double)__uint_as_float(h << 16) - x_top) * inv_t;
-                    mass = count * __double2ull_rn((K::bits(top) == h ? 1.0 : exp_of(y, sh.two_to)) * scale);
+                    for (int i = 0; i < 8; ++i) {          // (at most eight CTAs)
+                        x[i] = is && i < C ? *cluster.map_shared_rank(sh.count + at, i) : 0;
+                        y[i] = wide && i < C ? *cluster.map_shared_rank(m, i) : Sum{0, 0};
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { count[j] += x[i]; mass[j] += whole(y[i]); }
+                    to->all_count[b] = count[j];
+                    if (wide) to->all_mass[K::weighed(b)] = Sum{(uint32_t)mass[j], (uint32_t)(mass[j] >> 32)};
                 }
-                n = __reduce_add_sync(0xffffffffu, count);
-                mass = warp_total(mass);
+                any |= count[j] != 0;
             }
-            if (lane == 0) { to->step_count[s] = n; to->step_mass[s] = mass; }
+            if (__any_sync(0xffffffffu, any)) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    if constexpr (K::HALF) {
+                        const double y = ((double)__uint_as_float(h[j] << 16) - x_top) * inv_t;
+                        const unsigned long long w = count[j] * __double2ull_rn((K::bits(top) == h[j] ? 1.0 : exp_of(y, sh.two_to)) * scale);
+                        if (one[j]) mass[j] = w;
+                    }
+                    count[j] = __reduce_add_sync(0xffffffffu, count[j]);
+                    mass[j] = warp_total(mass[j]);
+                }
+            }
+            if (lane == 0)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    if (const int s = s0 + j * kWarps; s < K::STEPS) { to->step_count[s] = count[j]; to->step_mass[s] = mass[j]; }
         }
     }
     // the same for the parts, all of which are CTA 0's
@@ -381,8 +398,8 @@ struct Sampler {
                     else p.tie = p.count_at;                              // (one behind the last of them)
                 }
                 if (lane < C) of(lane)->place[turn] = p;
-                if (lane == 0) sh.found = 0;
             }
+            if (tid == 0) sh.found = 0;
             meet();
             p = sh.place[turn];
             turn ^= 1;
@@ -401,7 +418,7 @@ struct Sampler {
                     if (shift) add_to(&sh.part.mass[off], weight(d));
                 }
             });
-            if (C > 1) {
+            if (!kAlone) {
                 // to those of CTA 0 (few are not empty: the bin was one of thousands)
                 meet();
                 if (rank)
@@ -417,18 +434,35 @@ struct Sampler {
             if (rank == 0) { sum_parts(base, shift); __syncthreads(); }
         }
     }
-    // The same among the tokens of bin p.bin, of which there are few: CTA 0 gets a list of them
+    // The same among the tokens of bin p.bin, of which there are few: every CTA lists its own, CTA 0 takes them all
     __device__ Place ranked(Mode mode, unsigned long long y, const Place &p) {
-        Shared<T> *to = of(0);
+        const uint32_t size = K::end(p.bin) - p.d;
         mine([&](int i, uint32_t h) {
             const uint32_t d = K::key(h);
-            if (d == kNone || K::bin(d) != p.bin) return;
-            const uint32_t at = atomicAdd(&to->found, 1u);
-            if (at < kParts) { to->list.key[at] = d; to->list.id[at] = (uint32_t)i; }        // (it is: they have been counted)
+            if (d - p.d >= size) return;
+            const uint32_t at = atomicAdd(&sh.found, 1u);
+            if (at < kParts) { sh.list.key[at] = d; sh.list.id[at] = (uint32_t)i; }          // (it is: they have been counted)
         });
         meet();
         if (rank == 0) {
-            const uint32_t n = min(sh.found, (uint32_t)kParts);
+            uint32_t n = min(sh.found, (uint32_t)kParts), own = n;
+            if (!kAlone) {
+                const uint32_t upto = scan_sum(lane < C ? of(lane)->found : 0, lane);
+                n = min(__shfl_sync(0xffffffffu, upto, 31), (uint32_t)kParts);
+                uint32_t end[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) end[i] = __shfl_sync(0xffffffffu, upto, i);      // (at most eight CTAs)
+                for (uint32_t j = own + tid; j < n; j += kThreads) {
+                    int r = 0;
+                    uint32_t before = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) if (j >= end[i]) { r = i + 1; before = end[i]; }
+                    const Shared<T> *from = of(r);
+                    sh.list.key[j] = from->list.key[j - before];
+                    sh.list.id[j] = from->list.id[j - before];
+                }
+                __syncthreads();
+            }
             for (uint32_t j = tid; j < n; j += kThreads) sh.list.w[j] = weight(sh.list.key[j]);
             __syncthreads();
             // (up to n: BY_KEY asks for a place behind a key that may have no token)
@@ -515,7 +549,7 @@ struct Sampler {
             uint32_t mine = 0, all = 0;
 #pragma unroll
             for (int k = 0; k < kWarps; ++k) { if (k < warp) mine += sh.per_warp[k]; all += sh.per_warp[k]; }
-            if (C > 1) {
+            if (!kAlone) {
                 if (tid == 0) sh.found = all;
                 meet();
                 const uint32_t others = lane < C ? of(lane)->found : 0, sum = scan_sum(others, lane);
