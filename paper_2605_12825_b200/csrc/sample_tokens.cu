@@ -498,6 +498,13 @@ struct Sampler {
     // the largest key whose share is at least `least` (0 < least <= 1; the share falls as the key rises)
     __device__ uint32_t last_key(double least) const {
         unsigned long long lo = top, hi = sizeof(T) == 2 ? 0xffffu : 0xffffffffu;       // lo qualifies; hi does not (a NaN's place)
+        {
+            // it is almost always among the 32 keys around max + T ln(least)
+            const float x = (float)(x_top + (double)logf((float)least) / inv_t);
+            const unsigned long long g = K::key(__float_as_uint(x) >> (16 - K::LOW)), d0 = g > lo + 16 && g < hi ? g - 16 : lo, d = d0 + lane;
+            const int n = __popc(__ballot_sync(0xffffffffu, d < hi && share((uint32_t)d) >= least));
+            if (n > 0 && n < 32) return (uint32_t)d0 + n - 1;
+        }
 #pragma unroll 1
         while (hi - lo > 1) {
             const unsigned long long step = (hi - lo + 32) / 33, d = lo + step * (lane + 1);
