@@ -395,7 +395,7 @@ typedef struct {
     int32_t dtype;          /* orthrus_dtype_t of q, out, new K/V and pages         */
     int32_t page_size;      /* positions per page, a power of two up to 1024;
                                tensor-core path: from 16 on                         */
-    int32_t max_pages;      /* width of block_table; max_pages * page_size < 2^31   */
+    int32_t max_pages;      /* width of block_table; at most 2^31 - 2^16 positions  */
     int64_t n_pages;        /* pages in the pool, < 2^31                            */
     void *k_pages;          /* device [n_pages][Hkv][page_size][d]                  */
     void *v_pages;          /* device [n_pages][Hkv][page_size][d]                  */
@@ -428,7 +428,7 @@ typedef struct {
  * n_free_in (in place); nothing else may overlap.  The results do not depend on any order of execution.
  *   cache_len, n_new, held_in, held_out, granted  device int32 [batch];  block_table  device int32 [batch][max_pages]
  *   free_list  device int32 [n_pages];  n_free_in, n_free_out  device int32 [1];  slot_map  device int64 [batch][max_new]
- * 1 <= batch <= 8192, page_size a power of two up to 1024, 1 <= max_new <= 2^24.  `workspace` (status word) may be
+ * 1 <= batch <= 8192, page_size a power of two up to 1024, max_pages * page_size <= 2^31 - 2^16, 1 <= max_new <= 2^24.  `workspace` (status word) may be
  * NULL.  One launch.
  */
 orthrus_status_t orthrus_page_tables(int32_t batch, int32_t page_size, int32_t n_pages, int32_t max_pages, int32_t max_new,

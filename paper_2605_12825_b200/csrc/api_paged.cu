@@ -26,7 +26,8 @@ orthrus_status_t check_paged(const orthrus_paged_layer_t *L, bool attend)
     if (L->dtype != ORTHRUS_BF16 && L->dtype != ORTHRUS_FP32) return ORTHRUS_ERR_UNSUPPORTED;
     if (L->head_dim != 32 && L->head_dim != 64 && L->head_dim != 128 && L->head_dim != 256) return ORTHRUS_ERR_UNSUPPORTED;
     if (!page_size_ok(L->page_size) || L->block > (attend ? 64 : 1 << 20) || L->n_q_heads > 65535) return ORTHRUS_ERR_UNSUPPORTED;
-    if ((long long)L->max_pages * L->page_size > 0x7fffffffLL || L->n_pages > 0x7fffffffLL) return ORTHRUS_ERR_UNSUPPORTED;
+    // (a position and what a kernel adds to it to look ahead fit 31 bits)
+    if ((long long)L->max_pages * L->page_size > 0x7fff0000LL || L->n_pages > 0x7fffffffLL) return ORTHRUS_ERR_UNSUPPORTED;
     if (attend && (L->batch > 16384 || (long long)L->batch * L->n_kv_heads > (1 << 24))) return ORTHRUS_ERR_UNSUPPORTED;
     if ((long long)L->batch * L->block > 0x7fffffffLL) return ORTHRUS_ERR_UNSUPPORTED;
     return ORTHRUS_OK;
@@ -50,7 +51,9 @@ orthrus_status_t attend(const orthrus_paged_layer_t *L, int causal, const void *
         !aligned(L->block_table, 4) || !aligned(L->cache_len, 4) || !aligned(L->n_new, 4))
         return ORTHRUS_ERR_INVALID_ARG;
     const bool tc = use_tc(*L);
-    if (ws_bytes < (size_t)kHeaderBytes + (tc ? paged_tc_workspace_bytes(*L) : 0)) return ORTHRUS_ERR_WORKSPACE;
+    if (!tc && !paged_simt_shape(*L)) return ORTHRUS_ERR_UNSUPPORTED;
+    // (the larger of the two kernels', so that a workspace of the size that callers are told serves either)
+    if (ws_bytes < orthrus_paged_attend_workspace_bytes(L)) return ORTHRUS_ERR_WORKSPACE;
     PagedParams p;
     p.q = q; p.k_pages = L->k_pages; p.v_pages = L->v_pages; p.table = L->block_table; p.cache_len = L->cache_len;
     p.n_new = L->n_new; p.out = out; p.status = static_cast<int32_t *>(ws);
@@ -64,7 +67,7 @@ orthrus_status_t attend(const orthrus_paged_layer_t *L, int causal, const void *
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     set_last_path(tc ? "tcgen05" : "simt");
     const cudaError_t e = tc ? launch_paged_attend_tc(p, *L, static_cast<unsigned char *>(ws) + kHeaderBytes, cs)
-                             : launch_paged_attend_simt(p, L->dtype, cs);
+                             : launch_paged_attend_simt(p, *L, static_cast<unsigned char *>(ws) + kHeaderBytes, cs);
     return e == cudaSuccess ? ORTHRUS_OK : ORTHRUS_ERR_CUDA;
 }
 
@@ -82,7 +85,7 @@ orthrus_status_t orthrus_page_tables(int32_t batch, int32_t page_size, int32_t n
 {
     if (batch < 1 || n_pages < 1 || max_pages < 1 || max_new < 1) return ORTHRUS_ERR_INVALID_ARG;
     if (batch > 8192 || !page_size_ok(page_size) || max_new > (1 << 24)) return ORTHRUS_ERR_UNSUPPORTED;
-    if ((long long)max_pages * page_size > 0x7fffffffLL) return ORTHRUS_ERR_UNSUPPORTED;
+    if ((long long)max_pages * page_size > 0x7fff0000LL) return ORTHRUS_ERR_UNSUPPORTED;
     const void *const all[] = {cache_len, n_new, held_in, held_out, block_table, free_list, n_free_in, n_free_out, granted};
     for (const void *x : all)
         if (!x || !aligned(x, 4)) return ORTHRUS_ERR_INVALID_ARG;
@@ -143,7 +146,8 @@ orthrus_status_t orthrus_paged_commit_len(const orthrus_paged_layer_t *layer, co
 size_t orthrus_paged_attend_workspace_bytes(const orthrus_paged_layer_t *layer)
 {
     if (check_paged(layer, true) != ORTHRUS_OK) return 0;
-    return kHeaderBytes + (paged_tc_shape(*layer) ? paged_tc_workspace_bytes(*layer) : 0);
+    const size_t tc = paged_tc_shape(*layer) ? paged_tc_workspace_bytes(*layer) : 0, simt = paged_simt_workspace_bytes(*layer);
+    return kHeaderBytes + (tc > simt ? tc : simt);
 }
 
 orthrus_status_t orthrus_paged_ar_attend(const orthrus_paged_layer_t *layer, const void *q, void *out, void *workspace,

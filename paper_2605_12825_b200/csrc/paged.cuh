@@ -38,7 +38,9 @@ struct PagedParams {
 int small_rows_knob();                      // ORTHRUS_TC_SMALL_ROWS: 0, 1, or -1 where it is not set
 bool simt_forced();                         // orthrus_set_path("simt")
 void set_last_path(const char *name);       // what orthrus_last_path() answers on this thread; a literal
-cudaError_t launch_paged_attend_simt(const PagedParams &p, int dtype, cudaStream_t st);
+bool paged_simt_shape(const orthrus_paged_layer_t &L);       // its grid can be launched
+size_t paged_simt_workspace_bytes(const orthrus_paged_layer_t &L);
+cudaError_t launch_paged_attend_simt(const PagedParams &p, const orthrus_paged_layer_t &L, void *ws_body, cudaStream_t st);
 bool paged_tc_shape(const orthrus_paged_layer_t &L);        // the tensor-core kernel serves this shape
 size_t paged_tc_workspace_bytes(const orthrus_paged_layer_t &L);
 cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_layer_t &L, void *ws_body, cudaStream_t st);
@@ -58,6 +60,23 @@ __device__ inline void paged_request(const PagedParams &p, int b, int &P, int &n
     n = min(max(n, 0), min(p.K, p.max_pos));
     bad |= P < 0 || P > p.max_pos - n;
     P = min(max(P, 0), p.max_pos - n);
+}
+
+// Pieces that have arrived of a unit that is cut over CTAs.  The counts are in the workspace's header behind the status word, six of five bits in
+// a word, because a workspace may serve calls of other shapes and kinds in between, which write anything to the rest of it.  They are zero
+// between calls.
+constexpr int kMostPieces = 31, kCounts = (kHeaderBytes / 4 - 1) * 6;
+// One more of the n pieces (at most kMostPieces) of count i: is it the last?  By one thread; releases what a barrier before has gathered of its
+// block's stores, acquires what the others have released.
+__device__ inline bool last_piece(int32_t *header, int i, int n)
+{
+    int32_t *word = header + 1 + i / 6;
+    const int shift = i % 6 * 5;
+    uint32_t before;
+    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;" : "=r"(before) : "l"(word), "r"(1u << shift) : "memory");
+    const bool last = (int)(before >> shift & 31) == n - 1;
+    if (last) atomicSub(reinterpret_cast<uint32_t *>(word), (uint32_t)n << shift);
+    return last;
 }
 
 cudaError_t launch_sample_tokens(const void *logits, int dtype, int rows, int vocab, long long stride, const float *temperature,

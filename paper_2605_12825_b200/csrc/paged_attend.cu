@@ -12,7 +12,7 @@
 // Work is cut by tiles of 64 keys, not by requests: all tiles of all units lie on one line, and CTA c of n takes the stretch
 // [c T / n, (c + 1) T / n).  Every CTA finds its stretch from the lengths themselves, so that the host needs no plan, a captured graph serves any
 // lengths, and a batch of unequal requests loads all SMs alike.  A unit that is cut leaves pieces (unnormalised sums with their
-// reference) in the workspace; the CTA that finishes last, by the unit's counter, joins them in the order of their keys, which fixes the result.
+// reference) in the workspace; the CTA that finishes last, by the unit's count, joins them in the order of their keys, which fixes the result.
 //
 // CTA of 192 threads, 113 KB of shared memory and 256 TMEM columns: two fit an SM, so that one's softmax overlaps the other's products, and the
 // next call's CTAs can be resident early.
@@ -355,11 +355,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 const int c0 = owner(s, x.unit0), n = owner(s, x.unit0 + x.tiles - 1) - c0 + 1;
                 bar_softmax();
                 if (tid == 0) {
-                    // (releases what the barrier's other threads have stored, acquires what the other CTAs have)
-                    int *counter = w.counter + (long long)x.b * U + x.u, before;
-                    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
-                    if (before == n - 1) *counter = 0;
-                    *last_flag = before == n - 1;
+                    *last_flag = last_piece(p.status, c0, n);         // (no other cut unit begins in CTA c0)
                 }
                 // The join of the CTA that is the last.  Where things lie does not depend on it; vectors of four columns, a row a lane of them
                 const int rs = rows > 1 ? 32 - __clz(rows - 1) : 0;                      // log2 of the rows, rounded up
@@ -505,7 +501,7 @@ int keys_plan(const orthrus_paged_layer_t &L)
 }
 
 // CTAs of a call, and what its workspace holds: from the shape and the host's bound on the lengths.
-struct Grid { int ctas, row_tiles, rows, most_pieces; size_t counters, bytes; };
+struct Grid { int ctas, row_tiles, rows, most_pieces; size_t bytes; };
 Grid plan(const orthrus_paged_layer_t &L)
 {
     Grid g;
@@ -516,16 +512,15 @@ Grid plan(const orthrus_paged_layer_t &L)
     const long long tiles = units * (((long long)max_len_of(L) + L.block + KT - 1) / KT);
     // Two CTAs an SM; one where wide units are cut into more pieces than tiles are worth (8 KV heads, 8 requests of 2000 keys, 64 and 128
     // rows 33.5 and 50 us at two, 30.5 and 40 at one; 4 rows 20.6 and 24.6; 32 requests of 1024 to 8192, 64 rows 111 and 147)
-    const long long most = (g.rows <= 16 || tiles >= 32LL * num_sms() ? 2LL : 1LL) * num_sms();
+    const long long sms = (g.rows <= 16 || tiles >= 32LL * num_sms() ? 2LL : 1LL) * num_sms(), most = sms < kCounts ? sms : kCounts;
     g.ctas = (int)(tiles < 1 ? 1 : tiles < most ? tiles : most);
     // pieces of a unit: what the join has room for, and no more than one CTA adds up in the time the others save
     int padded = 1;
     while (padded < g.rows) padded *= 2;
     const int room = (L.head_dim == 128 ? g.rows <= 64 ? Shape<128, 64>::JOIN : Shape<128, 128>::JOIN
                                         : g.rows <= 64 ? Shape<64, 64>::JOIN : Shape<64, 128>::JOIN) / (padded * 8);
-    g.most_pieces = room < 32 ? room : 32;
-    g.counters = (size_t)((units * 4 + 255) / 256 * 256);
-    g.bytes = g.counters + 2 * (size_t)g.ctas * piece_floats(g.rows, L.head_dim) * sizeof(float);
+    g.most_pieces = room < kMostPieces ? room : kMostPieces;
+    g.bytes = 2 * (size_t)g.ctas * piece_floats(g.rows, L.head_dim) * sizeof(float);
     return g;
 }
 }  // namespace
@@ -541,8 +536,7 @@ cudaError_t launch_paged_attend_tc(const PagedParams &p, const orthrus_paged_lay
     w.box_shift = p.page_shift < 6 ? p.page_shift : 6;
     w.rows = g.rows;
     w.most_pieces = g.most_pieces;
-    w.counter = static_cast<int *>(ws_body);
-    w.pieces = reinterpret_cast<float *>(static_cast<unsigned char *>(ws_body) + g.counters);
+    w.pieces = static_cast<float *>(ws_body);
     PagedMaps tm;
     const unsigned long long rows = (unsigned long long)L.n_pages * L.n_kv_heads * L.page_size;
     if (!page_map(p.k_pages, p.d, rows, 1u << w.box_shift, &tm.k) || !page_map(p.v_pages, p.d, rows, 1u << w.box_shift, &tm.v))

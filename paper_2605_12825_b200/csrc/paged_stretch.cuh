@@ -15,7 +15,6 @@ struct PagedWork {
     int box_shift;           // log2 of the rows of a TMA box: min(page, 64)
     int rows;                // query rows a piece holds: min(rows of a tile, K G)
     int most_pieces;         // pieces of a unit
-    int *counter;            // [unit]: pieces that are in
     float *pieces;           // [2 CTAs] pieces: an output [d / 4][rows][4], behind it [rows][2] (reference, sum)
 };
 
