@@ -95,31 +95,6 @@ struct SampleArgs {
     float *logprob;
 };
 
-// 2^(j / 32)
-__constant__ double kTwoTo[32] = {
-    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
-    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
-    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
-    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
-    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
-    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
-    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
-    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0,
-};
-// e^x for x <= 0, to a few units of 2^-53: x = n (ln 2 / 32) + r, the Taylor polynomial of degree 6 in r (its remainder is below 2^-57), times
-// 2^(n mod 32 / 32), and n / 32 added to the exponent.  (Below -700, and of NaN: 0.)  Here because the fp64 pipe is what the sums over bins
-// wait for, and this is half the instructions of a polynomial without a table (512 rows of 128256: 16 us of a call, and SUMS us).
-__device__ inline double exp_of(double x, const double *two_to)
-{
-    const double n = rint(fmax(x, -800.0) * 46.166241308446828384);       // (NaN: -800)
-    const double r = fma(n, -7.247021293269686e-19, fma(n, -0.02166084939249829, x));                      // (ln 2 / 32 as a double, and what it lacks)
-    const int k = (int)n;
-    double y = 1.0 / 720.0;
-    y = fma(y, r, 1.0 / 120.0); y = fma(y, r, 1.0 / 24.0); y = fma(y, r, 1.0 / 6.0); y = fma(y, r, 0.5); y = fma(y, r, 1.0); y = fma(y, r, 1.0);
-    y *= two_to[k & 31];
-    return x > -700.0 ? __hiloint2double(__double2hiint(y) + ((k >> 5) << 20), __double2loint(y)) : 0.0;
-}
-
 // A sum of 64 bits as two of 32 that atomics can add to
 struct Sum { uint32_t lo, hi; };
 __device__ inline void add_to(Sum *s, unsigned long long x) {
@@ -145,7 +120,6 @@ template <typename T> struct Shared {
     uint32_t step_count[Keys<T>::STEPS + 1 + kPartSteps + 1];
     Place place[2];
     uint32_t top, found, per_warp[16];
-    double two_to[32];                                   // 2^(j / 32)
     // CTA 0 of several: what all of them have counted (a launch of single CTAs leaves out the room for these)
     uint32_t all_count[Keys<T>::STEPS * 32];
     Sum all_mass[Keys<T>::WEIGHED];
@@ -194,8 +168,10 @@ struct Sampler {
 
     __device__ void meet() { if (!kAlone) cluster.sync(); else __syncthreads(); }
     __device__ Shared<T> *of(int r) { return !kAlone ? cluster.map_shared_rank(&sh, r) : &sh; }
-    __device__ double share(uint32_t d) const {            // exp((x - max) / T)
-        return d == top ? 1.0 : exp_of((K::value(d) - x_top) * inv_t, sh.two_to);
+    // exp((x - max) / T) of a value x that is not the largest.  (NaN, of infinities that cancel: 0)
+    __device__ double share_of(double x) const { return exp(fmax((x - x_top) * inv_t, -800.0)); }
+    __device__ double share(uint32_t d) const {
+        return d == top ? 1.0 : share_of(K::value(d));
     }
     __device__ unsigned long long weight(uint32_t d) const { return __double2ull_rn(share(d) * scale); }
 
@@ -295,8 +271,8 @@ struct Sampler {
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     if constexpr (K::HALF) {
-                        const double y = ((double)__uint_as_float(h[j] << 16) - x_top) * inv_t;
-                        const unsigned long long w = count[j] * __double2ull_rn((K::bits(top) == h[j] ? 1.0 : exp_of(y, sh.two_to)) * scale);
+                        const double x = (double)__uint_as_float(h[j] << 16);
+                        const unsigned long long w = count[j] * __double2ull_rn((K::bits(top) == h[j] ? 1.0 : share_of(x)) * scale);
                         if (one[j]) mass[j] = w;
                     }
                     count[j] = __reduce_add_sync(0xffffffffu, count[j]);
@@ -591,7 +567,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
     for (int i = tid; i < K::SLOTS; i += kThreads) sh.count[i] = 0;
     for (int i = tid; i < K::WEIGHED; i += kThreads) sh.mass[i] = Sum{0, 0};
     if (tid == 0) sh.top = kNone;
-    if (tid < 32) sh.two_to[tid] = kTwoTo[tid];
     pdl_begin();
     s.row = static_cast<const T *>(a.logits) + r * a.stride;
     const int per = (a.vocab + s.C - 1) / s.C;
