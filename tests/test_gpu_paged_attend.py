@@ -264,6 +264,76 @@ def test_another_stream():
     assert torch.equal(out.cpu(), want)
 
 
+@pytest.mark.parametrize("d,page,dtype", [(32, 16, BF16), (256, 16, BF16), (128, 1, BF16), (64, 4, F32), (128, 16, F32), (256, 32, F32)])
+@pytest.mark.parametrize("lens,hint", [([5000, 0, 63], 0), ([64, 65, 127], 4000), ([1, 2047, 3000], 3000), ([9001], 9001), ([700, 20], 5)])
+def test_plain_arithmetic_cut_over_the_keys(d, page, dtype, lens, hint):
+    B = len(lens)
+    case(B, 1, 6, 2, d, page, lens, dtype=dtype, hint=hint)
+    case(B, 3, 5, 1, d, page, lens, [3, 1, 2][:B], dtype=dtype, hint=hint)
+
+
+def test_plain_arithmetic_with_more_units_than_counts():
+    case(40, 4, 12, 6, 32, 16, [(37 * b) % 300 for b in range(40)], dtype=F32)
+    case(7, 64, 6, 2, 256, 16, [(97 * b) % 200 for b in range(7)])
+
+
+def test_plain_arithmetic_leaves_values_alone_that_a_row_does_not_see():
+    """Row 1 of the block is NaN and infinity throughout; row 0 does not see it."""
+    t = make(1, 2, 4, 2, 256, 16, BF16, [300], [2])
+    want = ref.attend(t["q"], t["k"].nan_to_num(), t["v"].nan_to_num(), t["table"], [300], [2], True)
+    page, row = int(t["table"][0, 301 // 16]), 301 % 16
+    t["k"][page, :, row], t["v"][page, :, row] = math.nan, math.inf
+    got, status = run(t, 4, True)
+    assert status == 0
+    check(got[:, :1], want[:, :1], [1], float(t["v"].float().nan_to_num(posinf=0.0).abs().max()), BF16)
+
+
+def test_calls_of_all_kinds_share_a_workspace():
+    """What one call leaves in a workspace does not touch the next one, of whatever shape or kind."""
+    from paper_2605_12825_b200 import binding as B
+    torch.manual_seed(3)
+    calls, size = [], 0
+    for shape in ((1, 1, 8, 2, 128, 16, BF16, [9000], [1]), (2, 1, 8, 2, 256, 16, BF16, [3000, 500], [1, 1]),
+                  (5, 4, 32, 8, 128, 64, BF16, [2000, 10, 777, 3500, 1], [4] * 5), (3, 1, 4, 2, 128, 16, F32, [2500, 1, 900], [1] * 3),
+                  (2, 64, 4, 2, 64, 32, BF16, [3001, 50], [64, 7])):
+        t = make(*shape)
+        d = {n: x.cuda() for n, x in t.items()}
+        layer = B.make_paged_layer(d["k"], d["v"], d["table"], d["len"], shape[2], shape[1], d["new"])
+        out = torch.zeros_like(d["q"])
+        size = max(size, B.orthrus_paged_attend_workspace_bytes(layer))
+        calls.append((layer, d, out))
+    kc, vc = (torch.randn(2, 2, 4096, 128, device="cuda").to(BF16) for _ in range(2))
+    plain = B.make_layer(kc, vc, torch.tensor([4000, 300], dtype=torch.int32, device="cuda"), 8, 16, 4000)
+    q, kb, vb = (torch.randn(2, 16, h, 128, device="cuda").to(BF16) for h in (8, 2, 2))
+    out = torch.zeros_like(q)
+    size = max(size, B.orthrus_attend_workspace_bytes(plain))
+    logits, draft = torch.randn(8, 16, 5000, device="cuda"), torch.zeros(8, 16, dtype=torch.int32, device="cuda")
+    counts = [torch.zeros(n, dtype=torch.int32, device="cuda") for n in ((8,), (8, 16), (8, 16), (8,))]
+    size = max(size, B.orthrus_consensus_workspace_bytes(8, 16, 5000))
+
+    def everything(ws_of):
+        results = []
+        for layer, d, o in calls:
+            o.zero_()
+            B.orthrus_paged_ar_attend(layer, d["q"], o, ws_of())
+            results.append(o.clone())
+        B.orthrus_ar_verify_attend(plain, q, kb, vb, out, ws_of())
+        B.orthrus_consensus_accept(logits, draft, *counts, ws_of())
+        results += [out.clone()] + [c.clone() for c in counts]
+        return results
+
+    want = everything(lambda: B.new_workspace(size))
+    ws = B.new_workspace(size)
+    for _ in range(3):
+        for a, b in zip(everything(lambda: ws), want):
+            assert torch.equal(a, b)
+    # what is in the workspace behind its header may be anything
+    ws.view(torch.uint8)[256:].fill_(0x5a)
+    for a, b in zip(everything(lambda: ws)[:5], want):
+        assert torch.equal(a, b)
+    assert B.orthrus_read_status(ws) == 0
+
+
 def test_pool_past_32_bits():
     """A pool of 5 GB whose last pages are used: element offsets and byte offsets pass 2^31 and 2^32."""
     from paper_2605_12825_b200 import binding as B
