@@ -467,12 +467,16 @@ orthrus_status_t orthrus_paged_commit_len(const orthrus_paged_layer_t *layer, co
  * of KV head hq / (Hq / Hkv):  out[b][i][hq] = softmax_j(q[b][i][hq] . key_j * scale) applied to value_j.
  * Rows i >= n are padding: they are not read and out keeps what it holds there.  q, out: [B][K][Hq][d].
  *
- * The work is cut evenly over the GPU whatever the lengths are: CTAs take equal ranges of the batch's tiles of keys, and
- * the last CTA of a request to finish joins its pieces, in their order, so that results are the same in every run.
+ * Long requests are cut over several CTAs, whose pieces are joined in the order of their keys: results are the same in
+ * every run.  Large calls are cut evenly over the GPU whatever the lengths are; max_len_hint is used where it is small.
+ * Unless ORTHRUS_LAYER_NO_EARLY_LAUNCH is set a call may look at lengths and tables ahead of the end of the call before it, and looks again
+ * then.  In a row's result a masked score counts for nothing, whatever the key holds.  A value of the block itself that is not finite may
+ * make NaN of all rows of its request and head, those that do not see it included.
  * A cache_len or n_new out of range is clamped (ORTHRUS_DEV_BAD_CACHE_LEN); a table entry outside the pool among those that
  * a request needs raises ORTHRUS_DEV_BAD_PAGE, is not followed, and leaves the request's outputs undefined.
  * Workspace: orthrus_paged_attend_workspace_bytes(layer), initialised by orthrus_workspace_init once.  It depends on the
- * shape and on max_len_hint, not on the lengths.  1 <= batch <= 16384.
+ * shape, on max_len_hint and on the device, not on the lengths.  Calls of other shapes and kinds on the same stream may share it.
+ * 1 <= batch <= 16384.
  */
 size_t orthrus_paged_attend_workspace_bytes(const orthrus_paged_layer_t *layer);
 orthrus_status_t orthrus_paged_ar_attend(const orthrus_paged_layer_t *layer, const void *q, void *out, void *workspace,
@@ -499,7 +503,7 @@ orthrus_status_t orthrus_paged_diffusion_attend(const orthrus_paged_layer_t *lay
  * where a running mass is within such steps of a border.
  *   logits  device [rows] rows of `vocab` elements, `row_stride` elements apart (>= vocab), bf16 or fp32
  *   temperature, top_p, min_p, u, logprob  device float [rows];  top_k, token  device int32 [rows]
- * 1 <= rows <= 2^20, 1 <= vocab <= 2^24.  No workspace.  One launch.
+ * 1 <= rows <= 2^20, 1 <= vocab <= 2^24.  No workspace.  One launch (for each 65535 rows).
  */
 orthrus_status_t orthrus_sample_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
         const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, const float *u,

@@ -10,7 +10,8 @@
 // held_in and n_free_in and the first write of their successors, which may be the same arrays.
 //
 // What bounds it: latency (lengths, scan, barrier, list, table: five dependent steps) for a decoding batch; for prompts the 8 bytes
-// a slot, which the CTAs of the cluster write.
+// a slot, which the CTAs of the cluster write.  256 requests that grow by 16 rows, 8.8 us; 64 prompts of up to 8191 rows in pages of 64, 14.4 us for
+// 4.2 MB of slots: one cluster's stores, which grow with the CTAs it may have.
 #include "paged.cuh"
 #include "tc_ptx.cuh"
 

@@ -492,9 +492,10 @@ int keys_plan(const orthrus_paged_layer_t &L)
 {
     const int G = L.n_q_heads / L.n_kv_heads, knob = small_rows_knob();
     if (knob == 0 || !keys_rows(L.head_dim, G, L.block)) return 0;
+    const int kb = keys_kb_rows(L.head_dim, G, L.block), tiles = (L.block + kb - 1) / kb;
+    if ((long long)L.n_kv_heads * tiles > 65535) return 0;                       // (a dimension of its grid)
     const int max_len = max_len_of(L), S = paged_keys_splits(L, max_len);
     if (S == 0 || knob > 0) return S;
-    const int kb = keys_kb_rows(L.head_dim, G, L.block), tiles = (L.block + kb - 1) / kb;
     const long long bytes = 4LL * L.head_dim * L.batch * L.n_kv_heads * tiles * max_len;
     if (bytes > (G * L.block <= 16 ? 200000000LL : 270000000LL) && L.batch * tiles > 1) return 0;
     return ((long long)max_len + L.block + KT - 1) / KT <= 24LL * S ? S : 0;
