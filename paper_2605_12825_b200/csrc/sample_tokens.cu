@@ -229,63 +229,77 @@ struct Sampler {
         if (one) { if (count) mass = count * weight(d); }
         else mass = whole(parts ? sh.part.mass[b] : !kAlone ? sh.all_mass[K::weighed(b)] : sh.mass[K::weighed(b)]);
     }
-    // Sums of groups of 32 bins to CTA 0, and, where there are several CTAs, of the bins themselves; groups shared out over warps and CTAs.  A
-    // warp has J groups under way together, since one's exponentials are a chain that it would wait for.
+    // Sums of groups of 32 bins to CTA 0.  One CTA a row: a thread a group, which it walks from a place of its lane's on, in another bank than
+    // the other lanes (a warp a group, summed by reductions, takes twice as long with four rows on an SM).
+    __device__ void sum_steps_alone() {
+#pragma unroll 1
+        for (int s = tid; s < K::STEPS; s += kThreads) {
+            const bool pos = s >= K::POS / 32 && s < K::NEAR / 32, neg = s >= K::NEG / 32 && s < K::END / 32;
+            uint32_t n = 0;
+            unsigned long long m = 0;
+            if (pos || neg) {
+                const int at0 = pos ? K::NEAR - 32 - s * 32 : K::FINE + (s * 32 - K::NEG);           // its slots, which follow one another
+#pragma unroll 4
+                for (int j = 0; j < 32; ++j) {
+                    const int at = at0 + ((j + lane) & 31);
+                    const uint32_t count = sh.count[at];
+                    if (count == 0) continue;
+                    n += count;
+                    if constexpr (K::HALF) {
+                        const uint32_t h = pos ? K::LO + at : 0x8000u + K::LO + (at - K::FINE);
+                        m += count * __double2ull_rn((K::bits(top) == h ? 1.0 : share_of((double)__uint_as_float(h << 16))) * scale);
+                    } else {
+                        m += whole(sh.mass[at]);
+                    }
+                }
+            } else {
+#pragma unroll 1
+                for (int b = s * 32; b < s * 32 + 3; ++b) {
+                    uint32_t count = 0;
+                    unsigned long long mass = 0;
+                    if (K::exists(b)) in_bin(false, b, K::first(b), K::one_value(b), count, mass);
+                    n += count;
+                    m += mass;
+                }
+            }
+            sh.step_count[s] = n;
+            sh.step_mass[s] = m;
+        }
+    }
+    // Several CTAs: a warp a group, groups shared out over all warps; the bins themselves go to CTA 0 too
     __device__ void sum_steps() {
-        constexpr int J = kAlone ? 2 : 1;
         Shared<T> *to = of(0);
 #pragma unroll 1
-        for (int s0 = rank * kWarps + warp; s0 < K::STEPS; s0 += J * C * kWarps) {
-            uint32_t count[J], h[J];
-            unsigned long long mass[J];
-            bool one[J], any = false;
+        for (int s = rank * kWarps + warp; s < K::STEPS; s += C * kWarps) {
+            const int b = s * 32 + lane;
+            // slot, and, of a fine bin of bf16, the value; groups are of one kind
+            const bool pos = s >= K::POS / 32 && s < K::NEAR / 32, neg = s >= K::NEG / 32 && s < K::END / 32, is = pos || neg || K::exists(b);
+            const int at = pos ? K::NEAR - 1 - b : neg ? K::FINE + (b - K::NEG) : is ? K::slot(b) : 0;
+            const bool one = is && (pos || neg ? K::HALF : K::one_value(b)), wide = is && !one;
+            uint32_t count = 0;
+            unsigned long long mass = 0;
+            const Sum *m = sh.mass + (wide ? K::weighed(b) : 0);
+            uint32_t x[8];
+            Sum y[8];
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int s = s0 + j * kWarps, b = s * 32 + lane;
-                // slot, and, of a fine bin of bf16, the value; groups are of one kind
-                const bool pos = s >= K::POS / 32 && s < K::NEAR / 32, neg = s >= K::NEG / 32 && s < K::END / 32;
-                const bool is = pos || neg || (s < K::STEPS && K::exists(b));
-                const int at = pos ? K::NEAR - 1 - b : neg ? K::FINE + (b - K::NEG) : is ? K::slot(b) : 0;
-                one[j] = is && (pos || neg ? K::HALF : K::one_value(b));
-                const bool wide = is && !one[j];
-                h[j] = pos ? K::LO + at : neg ? 0x8000u + K::LO + (at - K::FINE) : is ? K::bits(K::first(b)) : 0;
-                count[j] = 0;
-                mass[j] = 0;
-                if (kAlone) {
-                    if (is) count[j] = sh.count[at];
-                    if (wide) mass[j] = whole(sh.mass[K::weighed(b)]);
-                } else {
-                    const Sum *m = sh.mass + (wide ? K::weighed(b) : 0);
-                    uint32_t x[8];
-                    Sum y[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {          // (at most eight CTAs)
-                        x[i] = is && i < C ? *cluster.map_shared_rank(sh.count + at, i) : 0;
-                        y[i] = wide && i < C ? *cluster.map_shared_rank(m, i) : Sum{0, 0};
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { count[j] += x[i]; mass[j] += whole(y[i]); }
-                    to->all_count[b] = count[j];
-                    if (wide) to->all_mass[K::weighed(b)] = Sum{(uint32_t)mass[j], (uint32_t)(mass[j] >> 32)};
-                }
-                any |= count[j] != 0;
+            for (int i = 0; i < 8; ++i) {                  // (at most eight CTAs)
+                x[i] = is && i < C ? *cluster.map_shared_rank(sh.count + at, i) : 0;
+                y[i] = wide && i < C ? *cluster.map_shared_rank(m, i) : Sum{0, 0};
             }
-            if (__any_sync(0xffffffffu, any)) {
 #pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    if constexpr (K::HALF) {
-                        const double x = (double)__uint_as_float(h[j] << 16);
-                        const unsigned long long w = count[j] * __double2ull_rn((K::bits(top) == h[j] ? 1.0 : share_of(x)) * scale);
-                        if (one[j]) mass[j] = w;
-                    }
-                    count[j] = __reduce_add_sync(0xffffffffu, count[j]);
-                    mass[j] = warp_total(mass[j]);
+            for (int i = 0; i < 8; ++i) { count += x[i]; mass += whole(y[i]); }
+            to->all_count[b] = count;
+            if (wide) to->all_mass[K::weighed(b)] = Sum{(uint32_t)mass, (uint32_t)(mass >> 32)};
+            uint32_t n = 0;
+            if (__any_sync(0xffffffffu, count)) {
+                if (one) {
+                    const uint32_t h = pos ? K::LO + at : neg ? 0x8000u + K::LO + (at - K::FINE) : K::bits(K::first(b));
+                    mass = count * __double2ull_rn((K::bits(top) == h ? 1.0 : share_of((double)__uint_as_float(h << 16))) * scale);
                 }
+                n = __reduce_add_sync(0xffffffffu, count);
+                mass = warp_total(mass);
             }
-            if (lane == 0)
-#pragma unroll
-                for (int j = 0; j < J; ++j)
-                    if (const int s = s0 + j * kWarps; s < K::STEPS) { to->step_count[s] = count[j]; to->step_mass[s] = mass[j]; }
+            if (lane == 0) { to->step_count[s] = n; to->step_mass[s] = mass; }
         }
     }
     // the same for the parts, all of which are CTA 0's
@@ -659,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
         return;
     }
     s.meet();
-    s.sum_steps();
+    if constexpr (kThreads == 256) s.sum_steps_alone(); else s.sum_steps();
     s.meet();
     if (s.rank == 0 && s.warp == 0) {
         s.run_steps(false);
