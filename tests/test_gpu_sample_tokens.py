@@ -88,6 +88,33 @@ def test_mixed_scales_in_a_row(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+def test_mixed_scales_where_a_row_has_one_cta(dtype):
+    """As many rows as leave no SMs for clusters: bins of one value and of many, long stretches of ties."""
+    g = torch.Generator().manual_seed(16)
+    R, V = 100, 40000
+    x = torch.randn(R, V, generator=g) * 10.0 ** (torch.rand(R, V, generator=g) * 14 - 12)
+    x[:, ::7] = 0.0
+    x[::2, 5::3] = 0.25
+    t, k, p, m, u = settings(R, 17)
+    compare(x.to(dtype), t, [n * 100 for n in k], p, None, u)
+    compare(x.to(dtype), t, None, None, None, u)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [300, 9000])
+def test_min_p_and_temperature_at_their_ends(dtype, V):
+    g = torch.Generator().manual_seed(V)
+    x = (torch.randn(24, V, generator=g) * 3).to(dtype)
+    x[20:, 5] = math.inf
+    m = [1.0, 0.9999999, 0.5, 1e-3, 1e-30, 1e-38] * 4
+    t = [1.0, 1e-6, 1e6, 0.3, 7.0, 1e-20] * 2 + [1e-38, 1.0, 50.0, 1e30, 0.1, 2.0] * 2
+    u = torch.rand(24, generator=g).tolist()
+    compare(x, t, None, None, m, u, most_close=0.3)
+    token, _ = run(x.cuda(), t, None, None, m, u)
+    assert token[20:] == [5] * 4
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_ties_go_to_the_lowest_id(dtype):
     V = 1000
     flat = torch.full((7, V), 1.5).to(dtype)
