@@ -57,7 +57,10 @@ template <int HD, int QR> struct Shape {
                          DONE = QUERY + 1, DRAIN = DONE + 1, BARS = DRAIN + 1;
     static constexpr int OFF_MISC = OFF_BAR + BARS * 8, SMEM = OFF_MISC + 16;
     static constexpr uint32_t TM_S = HD, TM_COLS = 256;            // O, then two buffers of scores
-    // the join: references and sums of the pieces [piece][row], in the place of the query rows
+    // Up to half as many query rows as have a place: the next unit's go to the other half while this one's are in use, and its first scores follow the
+    // last product of this one.  AHEAD: bytes to the other half.  (256 requests of 100 to 500 keys AHEADFIGURES)
+    static constexpr int AHEAD_ROWS = QR == 64 ? 32 : 0, AHEAD = QSUB / 2;
+    // the join: references and sums of the pieces [piece][row], in the place of the unit's query rows: of all, or of half of each panel
     static constexpr int JOIN = PANELS * QSUB;
     static_assert(NSLOT >= 5 && 2 * (SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
 };
@@ -93,6 +96,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int U = p.Hkv * w.row_tiles, page = 1 << p.page_shift;
+    const bool ahead = w.rows <= C::AHEAD_ROWS;
     Stretch s;
     Piece x;
     // tile number T of the CTA: K in ring item 2 T, V in 2 T + 1; item j in slot j % NSLOT
@@ -152,6 +156,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
         // ------------------------------------------------------------------ MMAs
         constexpr uint32_t IDESC_QK = make_idesc(KT, 0, QR), IDESC_PV = make_idesc(HD, 1, QR);
         const uint64_t q_desc = make_desc(sbase + C::OFF_Q, 16, 1024);
+        uint32_t q_at = 0;                               // the unit's query rows, in 16 bytes
         bool ok = true;
 #pragma unroll 1
         for (bool again = false; ; again = true) {
@@ -169,7 +174,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 const uint32_t d = tmem + C::TM_S + (T & 1) * KT;
 #pragma unroll
                 for (int kk = 0; kk < HD / 16; ++kk)
-                    umma_ss(d, q_desc + (((kk >> 2) * C::QSUB + (kk & 3) * 32) >> 4), kd + (((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4), IDESC_QK, kk > 0);
+                    umma_ss(d, q_desc + q_at + (((kk >> 2) * C::QSUB + (kk & 3) * 32) >> 4), kd + (((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4), IDESC_QK, kk > 0);
                 umma_commit(bar(C::EMPTY + slot));
                 umma_commit(bar(C::SCORES + (T & 1)));
             }
@@ -203,6 +208,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 __syncwarp();
             }
             ++units;
+            if (ahead) q_at ^= C::AHEAD >> 4;
         }
         if (*abort_flag) {                              // the MMAs in flight, before their operands and tensor memory go
             if (elect_one()) umma_commit(bar(C::DRAIN));
@@ -213,36 +219,49 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
         // ------------------------------------------------------------------ softmax
         const int r = lane < C::EACH ? warp * C::EACH + lane : MROWS;                    // (MROWS: none)
         const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
-        int T = 0, units = 0, h, r0, keys, rows;
-        long long at;
-        auto open = [&] {                                // the unit, and this thread's query row
-            const int M = x.n * p.G;
-            h = x.u / w.row_tiles, r0 = (x.u - h * w.row_tiles) * MROWS, keys = x.P + x.n;
-            rows = max(0, min(MROWS, M - r0));
-            at = r < rows ? row_offset(p, x.b, h, r0 + r, HD) : 0;
+        int T = 0, units = 0;
+        struct Rows { int h, r0, rows; long long at; };  // of a unit; `at`: this thread's query row
+        auto open = [&](const Piece &x, uint32_t place) {
+            Rows u;
+            u.h = x.u / w.row_tiles, u.r0 = (x.u - u.h * w.row_tiles) * MROWS;
+            u.rows = max(0, min(MROWS, x.n * p.G - u.r0));
+            u.at = r < u.rows ? row_offset(p, x.b, u.h, u.r0 + r, HD) : 0;
             // into swizzled panels of 64 columns; a row that does not exist is left as it is
-            const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(p.q) + at;
-            const uint32_t dst = sbase + C::OFF_Q + r * 128;
-            if (r < rows)
+            const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(p.q) + u.at;
+            const uint32_t dst = sbase + C::OFF_Q + place + r * 128;
+            if (r < u.rows)
 #pragma unroll
                 for (int c = 0; c < HD / 8; ++c)
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (c >> 3) * C::QSUB + (((c & 7) ^ (r & 7)) << 4)), "l"(src + c * 8) : "memory");
+            return u;
         };
-        bool have = false, ok = true;
-#pragma unroll 1
-        for (int look = 0; ; ++look) {                   // first and second look at the lengths, then unit after unit
-            if (look < 2) s = find_stretch(p, U, w.most_pieces);
-            have = next_piece(p, s, lane, x);
-            if (look == 0) griddep_wait();
-            if (have) open();
-            if (look == 0 && !still_so(p, s, lane)) { asm volatile("cp.async.wait_all;" ::: "memory"); continue; }
-            if (look == 0) look = 1;
-            if (!have) break;
-            const bool at_work = warp * C::EACH < rows;       // (other warps have padding only)
+        auto opened = [&] {                              // the rows are there
             asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::QUERY));
+        };
+        Piece y;                                         // the next unit, and its rows
+        Rows next;
+        uint32_t place = 0;                              // of this unit's rows
+        bool have = false, ok = true;
+#pragma unroll 1
+        for (int look = 0; ; ++look) {                   // first and, if they have changed, second look at the lengths
+            s = find_stretch(p, U, w.most_pieces);
+            have = next_piece(p, s, lane, x);
+            if (look == 0) griddep_wait();
+            if (have) next = open(x, 0);
+            if (look > 0 || still_so(p, s, lane)) break;
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        }
+        if (have) opened();
+#pragma unroll 1
+        while (have) {
+            const int h = next.h, r0 = next.r0, rows = next.rows, keys = x.P + x.n;
+            const long long at = next.at;
+            const bool at_work = warp * C::EACH < rows;       // (other warps have padding only)
+            have = next_piece(p, s, lane, y);
+            if (ahead && have) next = open(y, place ^ C::AHEAD);
             const int sees = p.causal ? min(keys, x.P + (r0 + r) / p.G + 1) : keys;
             float ref = -INFINITY, l = 0.f;
             for (int t = x.t0; t < x.t1; ++t, ++T) {
@@ -313,6 +332,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::PROBS + (T & 1)));
             }
+            if (ok && ahead && have) opened();
             if (ok) ok = mbar_wait_warp_call(bar(C::DONE), units & 1, abort_flag);
             ++units;
             ok = bar_softmax_and(ok);              // (a warp whose wait ran out has come here too: all leave together)
@@ -364,10 +384,14 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                 auto piece = [&](int k) { return k ? others + 2 * k * step : first; };
                 bar_softmax();
                 if (*last_flag && rows > 0) {
-                    float2 *st = reinterpret_cast<float2 *>(smem + C::OFF_Q);            // [piece][row]: references and sums, in the query rows' place
+                    // [piece][row]: references and sums, in the place of the unit's query rows
+                    auto st = [&](int e) -> float2 & {
+                        const int to = ahead ? place + (e * 8 / C::AHEAD) * C::QSUB + e * 8 % C::AHEAD : e * 8;
+                        return *reinterpret_cast<float2 *>(smem + C::OFF_Q + to);
+                    };
                     for (int e = tid; e < n << rs; e += 128) {
                         const int k = e >> rs, row = e & ((1 << rs) - 1);
-                        if (row < rows) st[e] = __ldcg(reinterpret_cast<const float2 *>(piece(k) + stats) + row);
+                        if (row < rows) st(e) = __ldcg(reinterpret_cast<const float2 *>(piece(k) + stats) + row);
                     }
                     // IT vectors of UN pieces under way together
                     auto sum_up = [&](auto it, auto un) {
@@ -400,7 +424,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
 #pragma unroll 4
                                     for (int k = 0; k < n; ++k)
 #pragma unroll
-                                        for (int i = 0; i < IT; ++i) top[i] = fmaxf(top[i], st[(k << rs) + row[i]].x);
+                                        for (int i = 0; i < IT; ++i) top[i] = fmaxf(top[i], st((k << rs) + row[i]).x);
 #pragma unroll
                                     for (int i = 0; i < IT; ++i) if (top[i] == -INFINITY) top[i] = 0.f;
                                 }
@@ -409,7 +433,7 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                                     if (k0 + u < n)
 #pragma unroll
                                         for (int i = 0; i < IT; ++i) {
-                                            const float2 rf = st[((k0 + u) << rs) + row[i]];
+                                            const float2 rf = st(((k0 + u) << rs) + row[i]);
                                             const float al = ex2(rf.x - top[i]);
                                             sum[i] = fmaf(rf.y, al, sum[i]);
                                             acc[i].x = fmaf(y[u][i].x, al, acc[i].x); acc[i].y = fmaf(y[u][i].y, al, acc[i].y);
@@ -428,10 +452,14 @@ paged_attend_tc_kernel(const __grid_constant__ PagedParams p, const __grid_const
                     };
                     if (vecs <= 256) sum_up(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
                     else sum_up(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
-                    bar_softmax();                         // (the references' place is the next query rows')
+                    bar_softmax();                         // (the references' place is query rows' again)
                 }
             }
+            x = y;
+            if (ahead) place ^= C::AHEAD;
+            else if (have) { next = open(x, 0); opened(); }
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -518,8 +546,9 @@ Grid plan(const orthrus_paged_layer_t &L)
     // pieces of a unit: what the join has room for, and no more than one CTA adds up in the time the others save
     int padded = 1;
     while (padded < g.rows) padded *= 2;
-    const int room = (L.head_dim == 128 ? g.rows <= 64 ? Shape<128, 64>::JOIN : Shape<128, 128>::JOIN
-                                        : g.rows <= 64 ? Shape<64, 64>::JOIN : Shape<64, 128>::JOIN) / (padded * 8);
+    const int place = L.head_dim == 128 ? g.rows <= 64 ? Shape<128, 64>::JOIN : Shape<128, 128>::JOIN
+                                        : g.rows <= 64 ? Shape<64, 64>::JOIN : Shape<64, 128>::JOIN;
+    const int room = (g.rows <= Shape<128, 64>::AHEAD_ROWS ? place / 2 : place) / (padded * 8);
     g.most_pieces = room < kMostPieces ? room : kMostPieces;
     g.bytes = 2 * (size_t)g.ctas * piece_floats(g.rows, L.head_dim) * sizeof(float);
     return g;
