@@ -6,8 +6,9 @@
 //      magnitude 2^-24 to 2^8 and zero have a bin each, what is outside shares four.  Weights are then needed once per value and not once per
 //      token (an exponential in double precision for a few thousand values instead of 150 thousand tokens).  fp32: bins of 2^16 neighbouring
 //      values, magnitudes 2^-8 to 2^8, which carry counts and the sum of their tokens' weights; the maximum is found by a pass before.
-//   2. Sums over groups of 32 bins go to one CTA, which finds the bin of each cut from them.
-//   3. A cut in a bin of many values: another pass lists the bin's tokens, which are ranked; if there are too many, it counts and weighs 1024
+//   2. Sums over groups of 32 bins go to one CTA, of which one warp finds the bin of each cut from them, one after the other (all CTAs at each
+//      cut, with a barrier between: 18.0 us for 16.3 with one row).
+//   3. A cut in a bin of many values needs all CTAs: another pass lists the bin's tokens, which are ranked; if there are too many, it counts and weighs 1024
 //      parts of the bin, until a part is one value.
 //   4. The wanted occurrence of the drawn value: a pass marks them in a bit map.
 // Weights are integers, exp((x - max) / T) in steps of 2^-S with 2^S times the vocabulary at most 2^62: sums do not depend on the
@@ -15,9 +16,9 @@
 //
 // What bounds it: one row, latency (its steps follow one another at the cluster's barriers); many rows, the atomics in shared memory (one
 // a token for bf16, three for fp32 next to an exponential in double): 32 lanes that count in banks of their own take 1.7 clocks of an SM,
-// in whatever banks their tokens have 4.0, and 512 rows give some SMs four.  One row of 151936 bf16: 17 us, of which the counts take 2, the sums over
-// bins 4, each filter 2, the token 3.4.  512 rows of 128256 bf16: 87 us, of which the counts take 45.  24 rows of
-// 32003 fp32 with top-p and min-p: 36 us.
+// in whatever banks their tokens have 4.0, and 512 rows give some SMs four.  One row of 151936 bf16: 16 us, of which the counts take 2, the sums over
+// bins 4, each filter 1, the token 3.4.  512 rows of 128256 bf16: 85 us, of which the counts take 45.  24 rows of
+// 32003 fp32 with top-p and min-p: 35 us.
 #include <cooperative_groups.h>
 #include <cmath>
 #include <cstddef>
@@ -109,6 +110,10 @@ __device__ inline unsigned long long whole(const Sum &s) { return (unsigned long
 // A place in the order: token number `tie` (from 0) of those with key d, which weigh w each; what is before them; its id, where that is known
 struct Place { uint32_t d, tie, count_before, count_at, id; int bin; unsigned long long mass_before, w; };
 
+enum Mode { BY_COUNT, BY_MASS, BY_KEY };
+// What CTA 0 tells the others: a cut that needs all of them, or the drawn token (stage 4)
+struct Order { Place at; unsigned long long y, mass; uint32_t cut; int stage; Mode mode; };
+
 constexpr int kPartSteps = kParts / 32;
 template <typename T> struct Shared {
     uint32_t count[Keys<T>::SLOTS + 3];                  // of a bin at its slot (in the end: the bit map)
@@ -122,13 +127,13 @@ template <typename T> struct Shared {
     unsigned long long step_mass[Keys<T>::STEPS + 1 + kPartSteps + 1];
     uint32_t step_count[Keys<T>::STEPS + 1 + kPartSteps + 1];
     Place place[2];
+    Order order;
     uint32_t top, found, per_warp[16];
     // CTA 0 of several: what all of them have counted (a launch of single CTAs leaves out the room for these)
     uint32_t all_count[Keys<T>::STEPS * 32];
     Sum all_mass[Keys<T>::WEIGHED];
 };
 
-enum Mode { BY_COUNT, BY_MASS, BY_KEY };
 
 __device__ inline uint32_t scan_sum(uint32_t x, int lane) {
 #pragma unroll
@@ -370,41 +375,24 @@ struct Sampler {
         p.count_at = __shfl_sync(0xffffffffu, count, l);
     }
 
-    // The place where the running count or mass passes y, or behind the last token with key at most y (BY_KEY).  All CTAs call it
-    // alike and learn the answer.
-    __device__ Place locate(Mode mode, unsigned long long y) {
-        Place p;
-        p.count_before = 0; p.mass_before = 0;
-        bool parts = false;
-        int shift = 0;
-        uint32_t base = 0;
+    // By one warp of CTA 0: which of the tokens with key p.d, of a bin or part that has no other
+    __device__ void settle(Mode mode, unsigned long long y, Place &p) const {
+        p.w = weight(p.d);
+        p.id = kNone;
+        p.tie = mode == BY_COUNT ? (uint32_t)(y - p.count_before)
+              : mode == BY_KEY ? p.count_at                              // (one behind the last of them)
+              : p.w ? (uint32_t)min((y - p.mass_before) / p.w, (unsigned long long)p.count_at - 1) : 0;
+    }
+    // The place where the running count or mass passes y, or behind the last token with key at most y (BY_KEY), of which bin p.bin is known, which
+    // has many values.  All CTAs call it alike and learn the answer.
+    __device__ Place refine(Mode mode, unsigned long long y, Place p) {
+        if (p.count_at <= kParts) return ranked(mode, y, p);
+        int shift = K::width(p.bin);
 #pragma unroll 1
         for (;;) {
-            if (rank == 0 && warp == 0) {
-                if (parts) run_steps(true);
-                search(parts, mode, y, shift, base, p);
-                const bool one = parts ? shift == 0 : K::one_value(p.bin);
-                p.w = one ? weight(p.d) : 0;
-                p.id = kNone;
-                // which of the tokens with this key
-                p.tie = 0;
-                if (one) {
-                    if (mode == BY_COUNT) p.tie = (uint32_t)(y - p.count_before);
-                    else if (mode == BY_MASS) p.tie = p.w ? (uint32_t)min((y - p.mass_before) / p.w, (unsigned long long)p.count_at - 1) : 0;
-                    else p.tie = p.count_at;                              // (one behind the last of them)
-                }
-                if (lane < C) of(lane)->place[turn] = p;
-            }
-            if (tid == 0) sh.found = 0;
-            meet();
-            p = sh.place[turn];
-            turn ^= 1;
-            if (parts ? shift == 0 : K::one_value(p.bin)) return p;
-            if (!parts && p.count_at <= kParts) return ranked(mode, y, p);
             // the bin's parts
-            base = p.d;
-            shift = max(0, (parts ? shift : K::width(p.bin)) - 10);
-            parts = true;
+            const uint32_t base = p.d;
+            shift = max(0, shift - 10);
             for (int i = tid; i < kParts; i += kThreads) { sh.part.count[i] = 0; sh.part.mass[i] = Sum{0, 0}; }
             __syncthreads();
             mine([&](int, uint32_t h) {
@@ -428,6 +416,16 @@ struct Sampler {
             }
             meet();
             if (rank == 0) { sum_parts(base, shift); __syncthreads(); }
+            if (rank == 0 && warp == 0) {
+                run_steps(true);
+                search(true, mode, y, shift, base, p);
+                if (shift == 0) settle(mode, y, p);
+                if (lane < C) of(lane)->place[turn] = p;
+            }
+            meet();
+            p = sh.place[turn];
+            turn ^= 1;
+            if (shift == 0) return p;
         }
     }
     // The same among the tokens of bin p.bin, of which there are few: every CTA lists its own, CTA 0 takes them all
@@ -601,6 +599,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
     const double u = fmin(fmax((double)a.u[r], 0.0), 1.0 - 0x1p-24);          // (NaN: 0)
     __syncthreads();
 
+    bool wait = true;                                 // there are counts or sums that other CTAs may still be at
     auto weigh = [&] { s.x_top = s.top == kNone ? 0.0 : K::value(s.top); };
     if constexpr (K::HALF) {
         if (tid == 0) sh.found = 0;
@@ -654,6 +653,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
             const uint32_t d = K::key(h);
             if (d != kNone && K::wide(K::bin(d))) add_to(&sh.mass[K::weighed(K::bin(d))], s.weight(d));
         };
+        if (!s.kAlone) wait = __any_sync(0xffffffffu, s.lane < s.C && s.of(s.lane)->found);
         if (listed <= 4 * kParts) for (uint32_t j = tid; j < listed; j += kThreads) weigh_one(sh.wide_bits[j]);
         else s.mine([&](int, uint32_t h) { weigh_one(h); });
     } else {
@@ -676,47 +676,66 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
         s.meet();
         return;
     }
-    s.meet();
+    if (wait) s.meet();
     if constexpr (kThreads == 256) s.sum_steps_alone(); else s.sum_steps();
     s.meet();
-    if (s.rank == 0 && s.warp == 0) {
-        s.run_steps(false);
-        if (s.lane > 0 && s.lane < s.C) {                 // (the others need the totals)
-            s.of(s.lane)->step_count[K::STEPS] = sh.step_count[K::STEPS];
-            s.of(s.lane)->step_mass[K::STEPS] = sh.step_mass[K::STEPS];
-        }
-    }
-    s.meet();
-    const uint32_t tokens = sh.step_count[K::STEPS];
-    unsigned long long mass = sh.step_mass[K::STEPS];
+    // Top-k, top-p, min-p, the draw.  One warp makes them one after the other as long as they fall into bins of one value.
+    const bool lead = s.rank == 0 && s.warp == 0;
     Place at;                                         // the last token that is kept, then the drawn one
-    uint32_t cut = kNone;                             // key of the former
-#pragma unroll 1
-    for (int stage = 0; stage < 4; ++stage) {         // top-k, top-p, min-p, the draw
-        Mode mode = BY_MASS;
-        unsigned long long y;
-        if (stage == 0) {
-            if (top_k <= 0 || (uint32_t)top_k >= tokens) continue;
-            mode = BY_COUNT;
-            y = (unsigned long long)top_k - 1;
-        } else if (stage == 1) {
-            if (!(top_p < 1.f)) continue;
-            const double want = ceil((double)fmaxf(top_p, 0.f) * (double)mass);
-            y = want < 1.0 ? 0 : (unsigned long long)want - 1;
-        } else if (stage == 2) {
-            if (!(min_p > 0.f)) continue;
-            if (min_p > 1.f) { mass = (unsigned long long)s.scale; continue; }        // the first token alone
-            const uint32_t d = s.last_key((double)min_p);
-            if (d >= cut) continue;
-            mode = BY_KEY;
-            y = d;
-        } else {
-            y = (unsigned long long)floor(u * (double)mass);
-        }
-        at = s.locate(mode, y);
-        if (stage == 3) break;
+    uint32_t tokens = 0, cut = kNone;                 // key of the former
+    unsigned long long mass = 0, y = 0;
+    int stage = 0;
+    Mode mode = BY_MASS;
+    if (lead) {
+        s.run_steps(false);
+        tokens = sh.step_count[K::STEPS];
+        mass = sh.step_mass[K::STEPS];
+    }
+    auto keep = [&] {
         mass = at.mass_before + ((unsigned long long)at.tie + (mode == BY_KEY ? 0 : 1)) * at.w;
         cut = at.d;
+    };
+#pragma unroll 1
+    for (;;) {
+        if (lead) {
+#pragma unroll 1
+            for (; stage < 4; ++stage) {
+                mode = BY_MASS;
+                if (stage == 0) {
+                    if (top_k <= 0 || (uint32_t)top_k >= tokens) continue;
+                    mode = BY_COUNT;
+                    y = (unsigned long long)top_k - 1;
+                } else if (stage == 1) {
+                    if (!(top_p < 1.f)) continue;
+                    const double want = ceil((double)fmaxf(top_p, 0.f) * (double)mass);
+                    y = want < 1.0 ? 0 : (unsigned long long)want - 1;
+                } else if (stage == 2) {
+                    if (!(min_p > 0.f)) continue;
+                    if (min_p > 1.f) { mass = (unsigned long long)s.scale; continue; }        // the first token alone
+                    const uint32_t d = s.last_key((double)min_p);
+                    if (d >= cut) continue;
+                    mode = BY_KEY;
+                    y = d;
+                } else {
+                    y = (unsigned long long)floor(u * (double)mass);
+                }
+                at.count_before = 0;
+                at.mass_before = 0;
+                s.search(false, mode, y, 0, 0, at);
+                if (!K::one_value(at.bin)) break;
+                s.settle(mode, y, at);
+                if (stage < 3) keep();
+            }
+            if (s.lane < s.C) s.of(s.lane)->order = Order{at, y, mass, cut, stage, mode};
+        }
+        if (tid == 0) sh.found = 0;
+        s.meet();
+        at = sh.order.at; y = sh.order.y; mass = sh.order.mass; cut = sh.order.cut; stage = sh.order.stage; mode = sh.order.mode;
+        if (stage == 4) break;
+        at = s.refine(mode, y, at);
+        if (stage == 3) break;
+        keep();
+        ++stage;
     }
     const Place drawn = at;
     if (drawn.id == kNone) s.find_token(drawn, a.token + r);
