@@ -128,7 +128,7 @@ template <typename T> struct Shared {
     uint32_t step_count[Keys<T>::STEPS + 1 + kPartSteps + 1];
     Place place[2];
     Order order;
-    uint32_t top, found, per_warp[16];
+    uint32_t top, found, per_warp[32];
     // CTA 0 of several: what all of them have counted (a launch of single CTAs leaves out the room for these)
     uint32_t all_count[Keys<T>::STEPS * 32];
     Sum all_mass[Keys<T>::WEIGHED];
@@ -159,11 +159,11 @@ __device__ inline unsigned long long warp_total(unsigned long long x) {
     return lo + (mid << 24) + (hi << 48);
 }
 
-template <typename T, int kThreads>
+// kAlone: one CTA a row
+template <typename T, int kThreads, bool kAlone>
 struct Sampler {
     using K = Keys<T>;
     static constexpr int kWarps = kThreads / 32;
-    static constexpr bool kAlone = kThreads == 256;       // one CTA a row
     Shared<T> &sh;
     const SampleArgs &a;
     cg::cluster_group cluster;
@@ -224,8 +224,13 @@ struct Sampler {
         return __reduce_min_sync(0xffffffffu, x);
     }
     __device__ void find_top() {
-        uint32_t best = kNone;
-        mine([&](int, uint32_t h) { best = min(best, K::key(h)); });
+        float high = -INFINITY;                            // (NaN is passed over)
+        vectors<4>(e0, e1,
+                [&](int, const uint4 &u) {
+                    high = fmaxf(high, fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w))));
+                },
+                [&](int, uint32_t h) { high = fmaxf(high, __uint_as_float(h)); });
+        uint32_t best = K::key(__float_as_uint(high));
         best = __reduce_min_sync(0xffffffffu, best);
         if (lane == 0) atomicMin(&sh.top, best);
     }
@@ -577,14 +582,14 @@ struct Sampler {
     }
 };
 
-template <typename T, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4 : 3) : 1) sample_tokens_kernel(const SampleArgs a)
+template <typename T, int kThreads, bool kAlone>
+__global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : Keys<T>::HALF ? 4 : 3) sample_tokens_kernel(const SampleArgs a)
 {
     using K = Keys<T>;
     extern __shared__ __align__(16) unsigned char smem[];
     Shared<T> &sh = *reinterpret_cast<Shared<T> *>(smem);
     const int tid = threadIdx.x;
-    Sampler<T, kThreads> s{sh, a, cg::this_cluster()};
+    Sampler<T, kThreads, kAlone> s{sh, a, cg::this_cluster()};
     s.C = gridDim.x; s.rank = blockIdx.x; s.turn = 0;
     s.tid = tid; s.lane = tid & 31; s.warp = tid >> 5;
     const int r = blockIdx.y;
@@ -659,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
             const uint32_t d = K::key(h);
             if (d != kNone && K::wide(K::bin(d))) add_to(&sh.mass[K::weighed(K::bin(d))], s.weight(d));
         };
-        if (!s.kAlone) wait = __any_sync(0xffffffffu, s.lane < s.C && s.of(s.lane)->found);
+        if (!kAlone) wait = __any_sync(0xffffffffu, s.lane < s.C && s.of(s.lane)->found);
         if (listed <= 4 * kParts) for (uint32_t j = tid; j < listed; j += kThreads) weigh_one(sh.wide_bits[j]);
         else s.mine([&](int, uint32_t h) { weigh_one(h); });
     } else {
@@ -667,15 +672,39 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
         s.meet();
         s.top = s.top_of_all();
         weigh();
-        const auto add = [&](uint32_t h) {
-            const uint32_t d = K::key(h);
-            if (d == kNone) return;
-            const int b = K::bin(d);
-            atomicAdd(&sh.count[K::slot(b)], 1u);
-            const unsigned long long w = s.weight(d);
-            if (w) add_to(&sh.mass[K::weighed(b)], w);
+        // tokens whose exponentials and atomics are under way together
+        const auto add = [&](auto n, const uint32_t (&h)[4]) {
+            constexpr int N = decltype(n)::value;
+            unsigned long long w[N];
+            Sum *to[N];
+            uint32_t carry[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const uint32_t d = K::key(h[j]);
+                w[j] = 0;
+                to[j] = sh.mass;
+                if (d == kNone) continue;
+                const int b = K::bin(d);
+                atomicAdd(&sh.count[K::slot(b)], 1u);
+                to[j] = sh.mass + K::weighed(b);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const uint32_t d = K::key(h[j]);
+                const unsigned long long x = s.weight(d == kNone ? s.top : d);
+                w[j] = d == kNone ? 0 : x;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) carry[j] = w[j] ? atomicAdd(&to[j]->lo, (uint32_t)w[j]) : 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const uint32_t hi = (uint32_t)(w[j] >> 32) + (carry[j] + (uint32_t)w[j] < carry[j]);
+                if (hi) atomicAdd(&to[j]->hi, hi);
+            }
         };
-        s.template vectors<2>(s.e0, s.e1, [&](int, const uint4 &u) { add(u.x); add(u.y); add(u.z); add(u.w); }, [&](int, uint32_t h) { add(h); });
+        s.template vectors<2>(s.e0, s.e1,
+                  [&](int, const uint4 &u) { const uint32_t h[4] = {u.x, u.y, u.z, u.w}; add(std::integral_constant<int, 4>(), h); },
+                  [&](int, uint32_t x) { const uint32_t h[4] = {x, x, x, x}; add(std::integral_constant<int, 1>(), h); });
     }
     if (s.top == kNone) {
         if (s.rank == 0 && tid == 0) { a.token[r] = 0; if (a.logprob) a.logprob[r] = NAN; }
@@ -683,7 +712,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
         return;
     }
     if (wait) s.meet();
-    if constexpr (kThreads == 256) s.sum_steps_alone(); else s.sum_steps();
+    if constexpr (kAlone) s.sum_steps_alone(); else s.sum_steps();
     s.meet();
     // Top-k, top-p, min-p, the draw.  One warp makes them one after the other as long as they fall into bins of one value.
     const bool lead = s.rank == 0 && s.warp == 0;
@@ -750,12 +779,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? (Keys<T>::HALF ? 4
         a.logprob[r] = (float)((drawn.d == s.top ? 0.0 : (K::value(drawn.d) - s.x_top) * s.inv_t) - log((double)mass / s.scale));
 }
 
-template <typename T, int kThreads>
+template <typename T, int kThreads, bool kAlone>
 cudaError_t launch_one(const SampleArgs &a, int rows, int C, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
     const size_t smem = C > 1 ? sizeof(Shared<T>) : offsetof(Shared<T>, all_count);
-    const cudaError_t e = configure(sample_tokens_kernel<T, kThreads>, done, (int)smem, false);
+    const cudaError_t e = configure(sample_tokens_kernel<T, kThreads, kAlone>, done, (int)smem, false);
     if (e != cudaSuccess) return e;
     for (int r0 = 0; r0 < rows; r0 += 65535) {               // (what a grid's second dimension holds)
         const int n = rows - r0 < 65535 ? rows - r0 : 65535;
@@ -766,18 +795,23 @@ cudaError_t launch_one(const SampleArgs &a, int rows, int C, cudaStream_t st)
         if (b.top_p) b.top_p += r0;
         if (b.min_p) b.min_p += r0;
         if (b.logprob) b.logprob += r0;
-        const cudaError_t x = launch_clusters(true, C, sample_tokens_kernel<T, kThreads>, dim3(C, n), kThreads, smem, st, b);
+        const cudaError_t x = launch_clusters(true, C, sample_tokens_kernel<T, kThreads, kAlone>, dim3(C, n), kThreads, smem, st, b);
         if (x != cudaSuccess) return x;
     }
     return cudaSuccess;
 }
 
-// CTAs per row: several while they find SMs of their own and have something to count
+// CTAs per row: several while they find SMs of their own and have something to count.  fp32 rows with an SM of their own have all its threads,
+// which wait for exponentials and atomics (75 rows of 128256 297 us with 256 threads, 127 with 1024; 148 of 32000 79 and 38).  bf16 rows
+// gain little (36.9 and 34.3; 75 of 8000 13.3 and 14.8) and keep to 256.
 template <typename T> cudaError_t launch_type(const SampleArgs &a, int rows, cudaStream_t st)
 {
     int C = 1;
     while (C < 8 && (long long)rows * C * 2 <= num_sms() && a.vocab / (C * 2) >= 2048) C *= 2;
-    return C > 1 ? launch_one<T, 512>(a, rows, C, st) : launch_one<T, 256>(a, rows, C, st);
+    if (C > 1) return launch_one<T, 512, false>(a, rows, C, st);
+    if constexpr (!Keys<T>::HALF)
+        if (rows <= num_sms()) return launch_one<T, 1024, true>(a, rows, 1, st);
+    return launch_one<T, 256, true>(a, rows, 1, st);
 }
 
 }  // namespace
