@@ -441,8 +441,10 @@ struct Sampler {
     }
     // The same among the tokens of bin p.bin, of which there are few: every CTA lists its own, CTA 0 takes them all
     __device__ Place ranked(Mode mode, unsigned long long y, const Place &p) {
-        const uint32_t size = K::end(p.bin) - p.d;
+        const uint32_t size = K::end(p.bin) - p.d, like = K::bits(p.d);
+        const bool fine = !K::HALF && K::fine(p.bin);      // (the bits' leading half says it)
         mine([&](int i, uint32_t h) {
+            if (fine && (h ^ like) >> 16) return;
             const uint32_t d = K::key(h);
             if (d - p.d >= size) return;
             const uint32_t at = atomicAdd(&sh.found, 1u);
@@ -672,39 +674,46 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : Keys<T>::HALF ?
         s.meet();
         s.top = s.top_of_all();
         weigh();
-        // tokens whose exponentials and atomics are under way together
-        const auto add = [&](auto n, const uint32_t (&h)[4]) {
-            constexpr int N = decltype(n)::value;
-            unsigned long long w[N];
-            Sum *to[N];
-            uint32_t carry[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const uint32_t d = K::key(h[j]);
-                w[j] = 0;
-                to[j] = sh.mass;
-                if (d == kNone) continue;
-                const int b = K::bin(d);
-                atomicAdd(&sh.count[K::slot(b)], 1u);
-                to[j] = sh.mass + K::weighed(b);
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const uint32_t d = K::key(h[j]);
-                const unsigned long long x = s.weight(d == kNone ? s.top : d);
-                w[j] = d == kNone ? 0 : x;
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) carry[j] = w[j] ? atomicAdd(&to[j]->lo, (uint32_t)w[j]) : 0;
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const uint32_t hi = (uint32_t)(w[j] >> 32) + (carry[j] + (uint32_t)w[j] < carry[j]);
-                if (hi) atomicAdd(&to[j]->hi, hi);
-            }
+        const auto one = [&](uint32_t h) {
+            const uint32_t d = K::key(h);
+            if (d == kNone) return;
+            const int b = K::bin(d);
+            atomicAdd(&sh.count[K::slot(b)], 1u);
+            const unsigned long long w = s.weight(d);
+            if (w) add_to(&sh.mass[K::weighed(b)], w);
         };
-        s.template vectors<2>(s.e0, s.e1,
-                  [&](int, const uint4 &u) { const uint32_t h[4] = {u.x, u.y, u.z, u.w}; add(std::integral_constant<int, 4>(), h); },
-                  [&](int, uint32_t x) { const uint32_t h[4] = {x, x, x, x}; add(std::integral_constant<int, 1>(), h); });
+        // four tokens that are not far from zero, whose exponentials and atomics are under way together (what a token costs here is instructions)
+        const auto four = [&](const uint4 &u) {
+            const uint32_t h[4] = {u.x, u.y, u.z, u.w};
+            uint32_t at[4], far = 0, lo[4], old[4], hi[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t mag = h[j] & 0x7fffffff, lead = mag >> 16;
+                const bool neg = h[j] >> 31;
+                far |= lead >= K::HI;
+                // (below LO the slots of the bins near zero)
+                at[j] = lead >= K::LO ? lead - K::LO + (neg ? K::FINE : 0) : 2 * K::FINE + (mag == 0 ? 2 : neg ? 3 : 1);
+            }
+            if (far) {
+#pragma unroll 1
+                for (int j = 0; j < 4; ++j) one(j == 0 ? u.x : j == 1 ? u.y : j == 2 ? u.z : u.w);
+                return;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) atomicAdd(&sh.count[at[j]], 1u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned long long w = __double2ull_rn(s.share_of((double)__uint_as_float(h[j])) * s.scale);
+                lo[j] = (uint32_t)w;
+                hi[j] = (uint32_t)(w >> 32);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) old[j] = lo[j] ? atomicAdd(&sh.mass[at[j]].lo, lo[j]) : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (const uint32_t x = hi[j] + (old[j] + lo[j] < old[j])) atomicAdd(&sh.mass[at[j]].hi, x);
+        };
+        s.template vectors<2>(s.e0, s.e1, [&](int, const uint4 &u) { four(u); }, [&](int, uint32_t h) { one(h); });
     }
     if (s.top == kNone) {
         if (s.rank == 0 && tid == 0) { a.token[r] = 0; if (a.logprob) a.logprob[r] = NAN; }
