@@ -442,14 +442,26 @@ struct Sampler {
     // The same among the tokens of bin p.bin, of which there are few: every CTA lists its own, CTA 0 takes them all
     __device__ Place ranked(Mode mode, unsigned long long y, const Place &p) {
         const uint32_t size = K::end(p.bin) - p.d, like = K::bits(p.d);
-        const bool fine = !K::HALF && K::fine(p.bin);      // (the bits' leading half says it)
-        mine([&](int i, uint32_t h) {
-            if (fine && (h ^ like) >> 16) return;
+        auto list = [&](int i, uint32_t h) {
             const uint32_t d = K::key(h);
             if (d - p.d >= size) return;
             const uint32_t at = atomicAdd(&sh.found, 1u);
             if (at < kParts) { sh.list.key[at] = d; sh.list.id[at] = (uint32_t)i; }          // (it is: they have been counted)
-        });
+        };
+        if (!K::HALF && K::fine(p.bin))                    // (the bits' leading half says it)
+            vectors<4>(e0, e1,
+                    [&](int i0, const uint4 &u) {
+                        const uint32_t x = u.x ^ like, y = u.y ^ like, z = u.z ^ like, w = u.w ^ like;
+                        if (min(min(x, y), min(z, w)) >> 16) return;
+                        uint32_t m = (x >> 16 == 0) | (y >> 16 == 0) << 1 | (z >> 16 == 0) << 2 | (w >> 16 == 0) << 3;
+#pragma unroll 1
+                        for (; m; m &= m - 1) {
+                            const int k = __ffs(m) - 1;
+                            list(i0 + k, k == 0 ? u.x : k == 1 ? u.y : k == 2 ? u.z : u.w);
+                        }
+                    },
+                    list);
+        else mine(list);
         meet();
         if (rank == 0) {
             uint32_t n = min(sh.found, (uint32_t)kParts), own = n;
