@@ -18,7 +18,8 @@
 // a token for bf16, three for fp32 next to an exponential in double): 32 lanes that count in banks of their own take 1.7 clocks of an SM,
 // in whatever banks their tokens have 4.0, and 512 rows give some SMs four.  One row of 151936 bf16: 16 us, of which the counts take 2, the sums over
 // bins 4, each filter 1, the token 3.4.  512 rows of 128256 bf16: 84 us, of which the counts take 43.  24 rows of
-// 32003 fp32 with top-p and min-p: 35 us.
+// 32003 fp32 with top-p and min-p: 28 us; 300 of 128256: 269 us, most of it the pass that weighs every
+// token.
 #include <cooperative_groups.h>
 #include <cmath>
 #include <cstddef>
@@ -823,7 +824,7 @@ cudaError_t launch_one(const SampleArgs &a, int rows, int C, cudaStream_t st)
 }
 
 // CTAs per row: several while they find SMs of their own and have something to count.  fp32 rows with an SM of their own have all its threads,
-// which wait for exponentials and atomics (75 rows of 128256 297 us with 256 threads, 127 with 1024; 148 of 32000 79 and 38).  bf16 rows
+// which wait for exponentials and atomics (75 rows of 128256 163 us with 256 threads, 85 with 1024; 148 of 32000 46 and 29; 75 of 8000 16.1 and 14.0).  bf16 rows
 // gain little (36.9 and 34.3; 75 of 8000 13.3 and 14.8) and keep to 256.
 template <typename T> cudaError_t launch_type(const SampleArgs &a, int rows, cudaStream_t st)
 {
