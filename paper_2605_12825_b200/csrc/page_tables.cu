@@ -4,14 +4,13 @@
 // list of free ones follows from two sums over the requests before it, so that every result is fixed by the inputs:
 //   given back   free_list[n_free + (given by requests before) + k]             k = 0, 1, .. in page order
 //   taken        free_list[total - 1 - (taken by requests before) - k]          total = n_free + all that is given back
-// One cluster: every CTA works out both sums for all requests (a block scan; a few KB from L2), gives back its share of the
-// pages, meets the others at the cluster's barrier, and then hands out and maps its share: two phases in one launch, where two
-// launches would read the lengths twice and wait for one another through the stream.  The barrier also stands between the last read of
-// held_in and n_free_in and the first write of their successors, which may be the same arrays.
+// Every CTA works out both sums for all requests (a block scan; a few KB from L2) and then takes its share of pages and slots.  Nothing that a CTA
+// looks up is written by another one: a page that one request gives back and another takes is read where the former held it, and not in the
+// list.  Only counts that are brought up to date in place (held_out, n_free_out) have to wait until all CTAs have read them: those calls
+// are one cluster, with a barrier.
 //
-// What bounds it: latency (lengths, scan, barrier, list, table: five dependent steps) for a decoding batch; for prompts the 8 bytes
-// a slot, which the CTAs of the cluster write.  256 requests that grow by 16 rows, 8.8 us; 64 prompts of up to 8191 rows in pages of 64, 14.4 us for
-// 4.2 MB of slots: one cluster's stores, which grow with the CTAs it may have.
+// What bounds it: latency (lengths, scan, list, slots: dependent steps, and a launch); for prompts the 8 bytes a slot.  256 requests that grow by 16
+// rows 8.1 us, 64 prompts of up to 8191 rows in pages of 64 6.5 us (4.2 MB of slots); in one cluster, as in place, 8.8 and 14.4.
 #include "paged.cuh"
 #include "tc_ptx.cuh"
 
@@ -33,7 +32,7 @@ __device__ inline unsigned long long warp_scan(unsigned long long x, int lane)
     return x;
 }
 
-__global__ void __launch_bounds__(kThreads, 1) page_tables_kernel(const PageTablesParams p, int per)
+__global__ void __launch_bounds__(kThreads, 1) page_tables_kernel(const PageTablesParams p, int per, bool in_place)
 {
     extern __shared__ Entry entry[];
     __shared__ unsigned long long sum[2][kWarps];
@@ -101,26 +100,30 @@ __global__ void __launch_bounds__(kThreads, 1) page_tables_kernel(const PageTabl
     };
     const unsigned mine = rank * kThreads + tid, all = C * kThreads;
     const unsigned n_given = (unsigned)min(given, (unsigned long long)(p.n_pages - n_free));
-#pragma unroll 1
-    for (unsigned t = mine; t < n_given; t += all) {
+    // where page number t of those that are given back is
+    auto given_page = [&](unsigned t) -> const int32_t * {
         const int b = request_of(t, [&](int i) { const Entry &e = entry[i]; return e.gives + (e.need >= 0 ? max(e.held - e.need, 0) : 0); });
         const Entry e = entry[b];
-        p.free_list[n_free + t] = p.table[(long long)b * p.max_pages + e.need + (t - e.gives)];
-    }
-    cluster_sync_all();
-
-    auto taken = [&](unsigned t) { return __ldcg(p.free_list + (total - 1 - t)); };
+        return p.table + (long long)b * p.max_pages + e.need + (t - e.gives);
+    };
+#pragma unroll 1
+    for (unsigned t = mine; t < n_given; t += all) p.free_list[n_free + t] = __ldcg(given_page(t));
+    // where page number t of those that are taken, from the end of the list, is
+    auto taken = [&](unsigned t) -> const int32_t * {
+        const unsigned at = total - 1 - t;
+        if (at < (unsigned)n_free) return p.free_list + at;
+        return given_page(at - n_free);
+    };
 #pragma unroll 1
     for (unsigned t = mine; t < upto; t += all) {
         const int b = request_of(t, [&](int i) { return entry[i].takes; });
         const Entry e = entry[b];
-        p.table[(long long)b * p.max_pages + e.held + (t - (e.takes - (unsigned)(e.need - e.held)))] = taken(t);
+        p.table[(long long)b * p.max_pages + e.held + (t - (e.takes - (unsigned)(e.need - e.held)))] = __ldcg(taken(t));
     }
-    // The page of position pos of a request: one that it held, or one that it has just got.  (Both are asked for where they are: the table
-    // of this call's pages may still be on its way.)
+    // the page of position pos of a request: one that it held, or one that it gets
     auto page_of = [&](const Entry &e, const int32_t *held, int pos) {
         const int j = pos >> p.page_shift;
-        return j < e.held ? held + j : p.free_list + (total - 1 - (e.takes - (unsigned)(e.need - e.held) + (unsigned)(j - e.held)));
+        return j < e.held ? held + j : taken(e.takes - (unsigned)(e.need - e.held) + (unsigned)(j - e.held));
     };
     const int page_mask = (1 << p.page_shift) - 1;
     if (p.max_new >= kStretch) {
@@ -157,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) page_tables_kernel(const PageTabl
             if (i >= p.max_new) { i -= p.max_new; ++b; }
         }
     }
+    if (in_place) cluster_sync_all();
     for (int r = (int)mine; r < p.B; r += (int)all) {
         const Entry e = entry[r];
         p.granted[r] = e.need < 0 ? 0 : p.n_new[r];
@@ -171,13 +175,22 @@ cudaError_t launch_page_tables(const PageTablesParams &p, cudaStream_t st)
 {
     // CTAs by the slots to write
     const long long slots = (long long)p.B * p.max_new;
-    int C = slots <= 8192 ? 1 : slots <= 32768 ? 4 : 8;
-    if (slots > 131072 && clusters_resident(16, 1) > 0) C = 16;
+    const bool in_place = p.held_out == p.held_in || p.n_free_out == p.n_free_in;
+    int C;
+    if (in_place) {
+        C = slots <= 8192 ? 1 : slots <= 32768 ? 4 : 8;
+        if (slots > 131072 && clusters_resident(16, 1) > 0) C = 16;
+    } else {
+        const long long want = (slots + 2047) / 2048;
+        C = (int)(want < num_sms() ? want : num_sms());
+    }
     static std::atomic<uint64_t> done{0};
     const int smem = p.B * (int)sizeof(Entry);
     const cudaError_t e = configure(page_tables_kernel, done, 8192 * (int)sizeof(Entry), true);
     if (e != cudaSuccess) return e;
-    return launch_clusters(true, C, page_tables_kernel, dim3(C), kThreads, smem, st, p, (p.B + kThreads - 1) / kThreads);
+    const int per = (p.B + kThreads - 1) / kThreads;
+    return in_place ? launch_clusters(true, C, page_tables_kernel, dim3(C), kThreads, smem, st, p, per, true)
+                    : launch_clusters(true, 1, page_tables_kernel, dim3(C), kThreads, smem, st, p, per, false);
 }
 
 }  // namespace orthrus

@@ -15,7 +15,7 @@ def run(page, lens, new, held, table, free, n_free, max_new, in_place=False, str
     dev = lambda v, t=I32: torch.tensor(v, dtype=t, device="cuda")  # noqa: E731
     n = len(lens)
     h, f = dev(held), dev([n_free])
-    ho, fo = (h, f) if in_place else (dev([-7] * n), dev([-7]))
+    ho, fo = (h if in_place in (True, "held") else dev([-7] * n)), (f if in_place in (True, "free") else dev([-7]))
     tb, fl, gr = dev(table), dev(free), dev([-7] * n)
     slots = torch.full((n, max_new), -9, dtype=torch.int64, device="cuda")
     ws = B.new_workspace(256)
@@ -63,6 +63,16 @@ def test_against_the_plain_form(batch, page, len_max, new_max, done, in_place):
     rng = random.Random(batch * 7 + page)
     s = state(rng, batch, page, len_max, new_max, batch * (-(-new_max // page) + 1), done)
     compare(page, s, new_max, in_place=in_place)
+
+
+@pytest.mark.parametrize("in_place", ["held", "free"])
+@pytest.mark.parametrize("batch,page,len_max,new_max,done", [(40, 16, 3000, 700, 20), (600, 8, 300, 100, 300)])
+def test_one_of_the_counts_in_place(batch, page, len_max, new_max, done, in_place):
+    """Pages that one request gives back and another takes, with so many slots that several CTAs look them up."""
+    rng = random.Random(batch)
+    s = state(rng, batch, page, len_max, new_max, 3 + batch * (-(-new_max // page)) // 4, done)
+    compare(page, s, new_max, in_place=in_place)
+    compare(page, s, new_max)
 
 
 @pytest.mark.parametrize("spare", [0, 1, 3, 10, 30])
