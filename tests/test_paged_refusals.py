@@ -36,6 +36,19 @@ def test_attention(lib, bad, code):
     assert lib.orthrus_launch_count() == n0
 
 
+def test_positions_fit_31_bits_with_room(lib):
+    """max_pages * page_size up to 2^31 - 2^16: what a kernel adds to a position to look ahead does not overflow."""
+    size = lib.orthrus_paged_attend_workspace_bytes
+    assert size(layer(lib, page_size=1024, max_pages=(1 << 21) - 64)) >= 256
+    for width in ((1 << 21) - 63, 1 << 21, (1 << 31) - 1):
+        L = layer(lib, page_size=1024, max_pages=width)
+        assert size(L) == 0
+        assert lib.lib().orthrus_paged_ar_attend(ctypes.byref(L), 0x10000, 0x20000, 0x30000, 1 << 30, None) == 2
+    # a grid of the plain-arithmetic kernel that cannot be launched
+    L = layer(lib, dtype=1, batch=16384, n_kv_heads=1, n_q_heads=65535, block=64, k_pages=0x1000, v_pages=0x2000)
+    assert lib.lib().orthrus_paged_ar_attend(ctypes.byref(L), 0x10000, 0x20000, 0x30000, 1 << 40, None) == 2
+
+
 def test_attention_arguments(lib):
     f, L = lib.lib().orthrus_paged_ar_attend, layer(lib)
     assert f(None, 0x10000, 0x20000, 0x30000, 1 << 30, None) == 1
