@@ -437,7 +437,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
             const int a = 2 * t + (kt >> 6), j = kt & 63;     // this thread's half and key in it
             // rows below lo do not see the key (all, if the key does not exist)
             const int lo = j >= half_keys(a) ? NR
-                           : PAGED ? (p.causal ? ((a0 + a) * HALF + j - P - i0) * p.G : 0)
+                           : PAGED ? (p.causal ? rows_before_key((a0 + a) * HALF + j, P + i0, p.G) : 0)
                            : (!APART && a >= n_mine && p.causal ? (j - i0) * p.G : 0);
             const bool masks = __any_sync(0xffffffffu, lo > 0);
             if (u > 0) mbar_wait_warp_call(bar(C::BAR_PV + wg), (u - 1) & 1, abort_flag);   // P buffer and O^T at rest

@@ -62,6 +62,10 @@ __device__ inline void paged_request(const PagedParams &p, int b, int &P, int &n
     P = min(max(P, 0), p.max_pos - n);
 }
 
+// Query rows (G to a position, the first at position `pos0`) in front of the first that sees key `key` of a causal call; keys up to some 64
+// positions behind pos0.  All rows see a key of the prefix; how far in front it lies, times G, need not fit 31 bits.
+__host__ __device__ inline int rows_before_key(int key, int pos0, int G) { return key > pos0 ? (key - pos0) * G : 0; }
+
 // Pieces that have arrived of a unit that is cut over CTAs.  The counts are in the workspace's header behind the status word, six of five bits in
 // a word, because a workspace may serve calls of other shapes and kinds in between, which write anything to the rest of it.  They are zero
 // between calls.
