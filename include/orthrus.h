@@ -472,7 +472,7 @@ orthrus_status_t orthrus_paged_commit_len(const orthrus_paged_layer_t *layer, co
  * Unless ORTHRUS_LAYER_NO_EARLY_LAUNCH is set a call may look at lengths and tables ahead of the end of the call before it, and looks again
  * then.  In a row's result a masked score counts for nothing, whatever the key holds.  A value of the block itself that is not finite may
  * make NaN of all rows of its request and head, those that do not see it included.
- * A cache_len or n_new out of range is clamped (ORTHRUS_DEV_BAD_CACHE_LEN); a table entry outside the pool among those that
+ * A cache_len or n_new out of range, or beyond what the table holds, is clamped (ORTHRUS_DEV_BAD_CACHE_LEN); a table entry outside the pool among those that
  * a request needs raises ORTHRUS_DEV_BAD_PAGE, is not followed, and leaves the request's outputs undefined.
  * Workspace: orthrus_paged_attend_workspace_bytes(layer), initialised by orthrus_workspace_init once.  It depends on the
  * shape, on max_len_hint and on the device, not on the lengths.  Calls of other shapes and kinds on the same stream may share it.

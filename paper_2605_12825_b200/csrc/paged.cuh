@@ -55,9 +55,9 @@ bool page_map(const void *ptr, unsigned d, unsigned long long rows, unsigned box
 __device__ inline void paged_request(const PagedParams &p, int b, int &P, int &n, bool &bad)
 {
     P = __ldcg(p.cache_len + b);
-    n = p.n_new ? __ldcg(p.n_new + b) : p.K;
-    bad = n < 0 || n > p.K;
-    n = min(max(n, 0), min(p.K, p.max_pos));
+    const int given = p.n_new ? __ldcg(p.n_new + b) : p.K;
+    n = min(max(given, 0), min(p.K, p.max_pos));
+    bad = n != given;
     bad |= P < 0 || P > p.max_pos - n;
     P = min(max(P, 0), p.max_pos - n);
 }
