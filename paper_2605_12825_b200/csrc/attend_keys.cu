@@ -370,7 +370,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
         __syncwarp();
         if (lane < 2 * per_half && half < last && pos < keys) {
             const int j = pos >> pg.page_shift, k = j - (a0 * HALF >> pg.page_shift);
-            int page = k < kPagesHeld ? reinterpret_cast<const int *>(smem + C::OFF_PAGES)[k] : __ldg(pg.table + (long long)b * pg.max_pages + j);
+            int page = k < kPagesHeld ? reinterpret_cast<const int *>(smem + C::OFF_PAGES)[k] : __ldcg(pg.table + (long long)b * pg.max_pages + j);
             if (page < 0 || page >= pg.n_pages) {
                 if (p.status) atomicOr(p.status, ORTHRUS_DEV_BAD_PAGE);
                 page = 0;
@@ -739,7 +739,7 @@ __device__ __forceinline__ void attend_keys(const AttnParams &p, const KeysMaps 
             // this CTA's table entries, then as below, a whole warp
             const int *first = pg.table + (long long)b * pg.max_pages + (a0 * HALF >> pg.page_shift);
             const int n_held = min(kPagesHeld, nh > 0 ? ((min(a1 * HALF, keys) - 1) >> pg.page_shift) - (a0 * HALF >> pg.page_shift) + 1 : 0);
-            for (int k = lane; k < n_held; k += 32) reinterpret_cast<int *>(smem + C::OFF_PAGES)[k] = __ldg(first + k);
+            for (int k = lane; k < n_held; k += 32) reinterpret_cast<int *>(smem + C::OFF_PAGES)[k] = __ldcg(first + k);
             __syncwarp();
             const int n_items = 2 * n_tiles;
             bool ok = (sbase & 1023u) == 0;

@@ -125,10 +125,10 @@ __global__ void __launch_bounds__(NWARPS * 32) attend_mma_kernel(AttnParams p)
         const bool v0 = R0 < p.M, v1 = R1 < p.M;
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks) {
-            qf[ks][0] = v0 ? __ldg(q0 + ks * 8 + tq) : 0u;
-            qf[ks][1] = v1 ? __ldg(q1 + ks * 8 + tq) : 0u;
-            qf[ks][2] = v0 ? __ldg(q0 + ks * 8 + 4 + tq) : 0u;
-            qf[ks][3] = v1 ? __ldg(q1 + ks * 8 + 4 + tq) : 0u;
+            qf[ks][0] = v0 ? q0[ks * 8 + tq] : 0u;
+            qf[ks][1] = v1 ? q1[ks * 8 + tq] : 0u;
+            qf[ks][2] = v0 ? q0[ks * 8 + 4 + tq] : 0u;
+            qf[ks][3] = v1 ? q1[ks * 8 + 4 + tq] : 0u;
         }
     }
 

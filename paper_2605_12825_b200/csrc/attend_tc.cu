@@ -404,7 +404,7 @@ attend_tc_kernel(const AttnParams p, const __grid_constant__ TcMaps tm, const in
         bool bad = false;
 #pragma unroll 1
         for (int j = j_lo; j <= j_hi; ++j) {
-            const int a = __ldg(p.cache_len + (long long)b * p.nb + j);
+            const int a = __ldcg(p.cache_len + (long long)b * p.nb + j);
             bad |= a < 0 || a > len_hi;
             P = max(P, min(max(a, 0), len_hi));
         }
@@ -463,7 +463,7 @@ attend_tc_kernel(const AttnParams p, const __grid_constant__ TcMaps tm, const in
         if constexpr (PACK) {
             if (valid) {
                 const int j_row = i_row / p.kb_width;
-                a_row = min(max(__ldg(p.cache_len + (long long)b * p.nb + j_row), 0), len_hi);
+                a_row = min(max(__ldcg(p.cache_len + (long long)b * p.nb + j_row), 0), len_hi);
                 k0_row = j_row * p.kb_width;
             }
         }

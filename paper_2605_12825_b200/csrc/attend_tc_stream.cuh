@@ -174,7 +174,7 @@ attend_tc_stream_kernel(const AttnParams p, const __grid_constant__ TcMaps tm, c
         const int Pi = min(max(raw, 0), len_hi);
         int before = 0;
         for (int j = 0; j < p.B; ++j) {
-            const int Pj = min(max(__ldg(p.cache_len + j), 0), len_hi);
+            const int Pj = min(max(__ldcg(p.cache_len + j), 0), len_hi);
             before += (Pj > Pi) || (Pj == Pi && j < i);
         }
         s_seq[before] = (unsigned char)i;
@@ -203,7 +203,7 @@ attend_tc_stream_kernel(const AttnParams p, const __grid_constant__ TcMaps tm, c
         const long long within = g - (long long)p.Hkv * s_cum[r];
         pc.n = n; pc.h = (int)(within / n); pc.tl0 = (int)(within % n);
         pc.tl1 = (int)min((long long)n, pc.tl0 + (g_end - g));
-        pc.b = s_seq[r]; pc.P = min(max(__ldg(p.cache_len + pc.b), 0), len_hi); pc.unit = r * p.Hkv + pc.h;
+        pc.b = s_seq[r]; pc.P = min(max(__ldcg(p.cache_len + pc.b), 0), len_hi); pc.unit = r * p.Hkv + pc.h;
         pc.U0 = (long long)p.Hkv * s_cum[r] + (long long)pc.h * n;
         g += pc.tl1 - pc.tl0;
         return true;

@@ -82,7 +82,7 @@ static __device__ __noinline__ int rank_by_length(const AttnParams &p, int want,
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int i = lane + 32 * k;
-        len[k] = i < p.B ? min(max(__ldg(p.cache_len + i), 0), len_hi) : -1;
+        len[k] = i < p.B ? min(max(__ldcg(p.cache_len + i), 0), len_hi) : -1;
     }
     if (p.B <= 32) {
         int before = 0;
@@ -185,6 +185,8 @@ void count_launch(int n = 1);
 // reads or writes global memory: the wait returns when the preceding grid has completed (and with
 // it, because that grid waited too, everything before it), and only then may the next kernel be
 // placed.  Between two short kernels this takes the launch latency (about 1.5 us) out of the stream.
+// The kernel is there while the one before it still writes, so nothing is read by the read-only path (__ldg), which is for memory
+// that stays as it is for as long as a kernel lives.
 __device__ inline void pdl_begin()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");

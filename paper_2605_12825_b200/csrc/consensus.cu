@@ -65,9 +65,9 @@ __global__ void __launch_bounds__(256) argmax_partial_kernel(const T *logits, in
         const uint4 *vp = reinterpret_cast<const uint4 *>(rowp + body0);
         int v = threadIdx.x;
         for (; v + 3 * 256 < n_vec; v += 4 * 256) {
-            uint4 u[4];
+            uint4 u[4];                          // (past L1: 512 rows of 151936 bf16 28.3 us, by loads that L1 keeps 32.7)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = __ldg(vp + v + k * 256);
+            for (int k = 0; k < 4; ++k) u[k] = __ldcg(vp + v + k * 256);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 float x[N];
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(256) argmax_partial_kernel(const T *logits, in
         }
         for (; v < n_vec; v += 256) {
             float x[N];
-            Vec<T>::unpack(__ldg(vp + v), x);
+            Vec<T>::unpack(__ldcg(vp + v), x);
             const int i0 = body0 + v * N;
 #pragma unroll
             for (int e = 0; e < N; ++e)

@@ -145,7 +145,7 @@ template <typename T> __device__ __noinline__ VecOf<T> load_part(const T *row, i
 template <typename T> __device__ inline void load_vec(const T *row, const RowShape &s, int v, float (&x)[Elem<T>::N]) {
     const int i0 = v * Elem<T>::N - s.a;
     if (whole<T>(s, v)) {
-        Elem<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(row + i0)), x);
+        Elem<T>::unpack(*reinterpret_cast<const uint4 *>(row + i0), x);
     } else {
         const VecOf<T> r = load_part<T>(row, i0, s.V);
 #pragma unroll
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) sample_stats_kernel(const T *la, con
             for (; v + 96 < w1; v += 128) {
                 uint4 x[4], y[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) { x[q] = __ldg(va + v + q * 32); y[q] = __ldg(vd + v + q * 32); }
+                for (int q = 0; q < 4; ++q) { x[q] = va[v + q * 32]; y[q] = vd[v + q * 32]; }
                 float f[4][N];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) Elem<T>::unpack(x[q], f[q]);
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kThreads) sample_stats_kernel(const T *la, con
                 absorb<4, N>(d, f, c);
             }
             for (; v < w1; v += 32) {
-                const uint4 x = __ldg(va + v), y = __ldg(vd + v);
+                const uint4 x = va[v], y = vd[v];
                 float f[1][N];
                 Elem<T>::unpack(x, f[0]); absorb<1, N>(a, f, c);
                 Elem<T>::unpack(y, f[0]); absorb<1, N>(d, f, c);
@@ -378,8 +378,8 @@ __global__ void __launch_bounds__(kFinishThreads, 2) sample_finish_kernel(const 
         auto ask = [&](int r) {
             const int v = w0 + r * 32 + lane;
             if (r < rounds && v < w1 && whole<T>(sh, v)) {
-                nx = __ldg(reinterpret_cast<const uint4 *>(ra + v * N - sh.a));
-                ny = __ldg(reinterpret_cast<const uint4 *>(rd + v * N - sh.a));
+                nx = *reinterpret_cast<const uint4 *>(ra + v * N - sh.a);
+                ny = *reinterpret_cast<const uint4 *>(rd + v * N - sh.a);
             }
         };
         ask(0);

@@ -74,8 +74,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) paged_write_kerne
     // slot and position of an item's row, an item ahead
     auto look = [&](long long it, long long &slot, int &pos) {
         const long long row = it / a.chunks, b = row / a.K;
-        slot = __ldg(a.slot_map + row);
-        pos = ROPE ? max(__ldg(a.cache_len + b), 0) + (int)(row - b * a.K) : 0;
+        slot = a.slot_map[row];
+        pos = ROPE ? max(a.cache_len[b], 0) + (int)(row - b * a.K) : 0;
     };
     long long it = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), slot = -1, next_slot = -1;
     int pos = 0, next_pos = 0;

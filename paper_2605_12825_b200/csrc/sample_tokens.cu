@@ -194,7 +194,7 @@ struct Sampler {
         for (int v = tid; v < n; v += U * kThreads) {
             uint4 u[U];
 #pragma unroll
-            for (int q = 0; q < U; ++q) { const int i = min(v + q * kThreads, n - 1); u[q] = __ldg(x + (BACK ? n - 1 - i : i)); }
+            for (int q = 0; q < U; ++q) { const int i = min(v + q * kThreads, n - 1); u[q] = __ldcg(x + (BACK ? n - 1 - i : i)); }
 #pragma unroll
             for (int q = 0; q < U; ++q) {
                 const int i = v + q * kThreads;
@@ -203,7 +203,7 @@ struct Sampler {
         }
         // (at most N - 1 each, fewer than the threads)
         const int i = tid < head ? b + tid : tid - head < e - tail ? tail + tid - head : -1;
-        if (i >= 0) g(i, (uint32_t)__ldg(reinterpret_cast<const typename K::Raw *>(row) + i));
+        if (i >= 0) g(i, (uint32_t)reinterpret_cast<const typename K::Raw *>(row)[i]);
     }
     // f(element, bits) for this CTA's elements.  In little code: for what is not done for every row
     template <class F> __device__ void mine(F f) const {
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : Keys<T>::HALF ?
                           add(x); add(y); add(z); add(w);
                       } else {
 #pragma unroll 1
-                          for (int k = 0; k < K::N; ++k) rare((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(s.row) + i0 + k));
+                          for (int k = 0; k < K::N; ++k) rare((uint32_t)reinterpret_cast<const uint16_t *>(s.row)[i0 + k]);
                       }
                   },
                   [&](int, uint32_t h) { rare(h); });
