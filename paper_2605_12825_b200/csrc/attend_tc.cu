@@ -1035,7 +1035,7 @@ static cudaError_t launch_tc(const AttnParams &p, const TcMaps &tm, int kb, int 
 bool tc_stream_shape(int B, int G, int K) { return B <= STREAM_MAX_B && G >= 1 && G * K <= MROWS && K <= TN; }
 
 // Workspace of the persistent kernel behind the header: two partial tiles and their (max, sum)
-// rows per CTA, then one arrival counter per unit (zero between calls).
+// rows per CTA, then one arrival counter per unit (zero when the kernel starts and when it ends).
 size_t tc_stream_workspace_bytes(int B, int Hkv, int n_ctas)
 {
     return (size_t)n_ctas * 2 * (MROWS * HD * sizeof(float) + MROWS * 2 * sizeof(float)) +
@@ -1074,6 +1074,10 @@ cudaError_t launch_attend_tc_stream(const AttnParams &p, int n_ctas, void *ws_bo
     sa.part_o = reinterpret_cast<float4 *>(base);
     sa.part_ml = reinterpret_cast<float2 *>(base + (size_t)n_ctas * 2 * MROWS * HD * sizeof(float));
     sa.counters = reinterpret_cast<int32_t *>(base + (size_t)n_ctas * 2 * (MROWS * HD + MROWS * 2) * sizeof(float));
+    // The counters lie where calls of other shapes and kinds that share the workspace leave what they like.  (The kernel cannot clear them
+    // itself: its CTAs do not wait for one another before the first one arrives)
+    const cudaError_t cleared = cudaMemsetAsync(sa.counters, 0, (size_t)p.B * p.Hkv * sizeof(int32_t), st);
+    if (cleared != cudaSuccess) return cleared;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_ctas, 1, 1);
     cfg.blockDim = dim3(Shape<1>::NTHREADS);

@@ -49,7 +49,7 @@ static_assert(2 * (STREAM_SMEM_BYTES + 1024) <= 228 * 1024, "two CTAs per SM");
 struct StreamArgs {
     float4 *part_o;        // [G][2] partial tiles, each [32 chunks][128 rows] of 16 bytes
     float2 *part_ml;       // [G][2][128] (max, sum)
-    int32_t *counters;     // [B * Hkv] arrivals per unit; zero between calls
+    int32_t *counters;     // [B * Hkv] arrivals per unit; zero at the kernel's start and end
 };
 
 // first global tile of CTA c when T tiles are cut into G ranges
