@@ -1204,6 +1204,9 @@ int paged_keys_splits(const orthrus_paged_layer_t &L, int max_len)
     const long long units = (long long)L.batch * L.n_kv_heads * tiles;
     const int per_sm = nr <= 64 ? 2 : 1;
     if ((long long)L.n_kv_heads * tiles > 65535 || units > 2 * num_sms()) return 0;
+    // (Where the contiguous call would keep the block apart from the tiles, its split is taken here too, although the block is a part of
+    // them, since it is the faster one: 46 shapes of 1 to 15 units of 36 to 64 rows, 2304 to 8192 keys, at which the count with the block in the tiles
+    // gives another, by 4 % in the mean; 8 units of 64 rows and 4096 keys 11.8 us at 16 CTAs, 12.6 at 13)
     bool apart = false;
     const long long all = (long long)max_len + L.block - HALF;          // (as keys_splits counts: the block a half of its own)
     const int S = keys_splits(d, G, L.block, (int)units, all < 0 ? 0 : (int)all, &apart);
