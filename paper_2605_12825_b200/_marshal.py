@@ -149,6 +149,12 @@ def _space(t):
     return _paged(t, "workspace", torch.uint8, (-1,)), t.numel()
 
 
+def _here(layer):
+    """Of a layer made of tensors: they are on the current device."""
+    if layer.device is not None and layer.device != torch.cuda.current_device():
+        raise ValueError(f"layer: on cuda:{layer.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
 def _rows(layer):
     return torch.float32 if layer.dtype else torch.bfloat16
 
@@ -169,6 +175,7 @@ def page_tables(page_size, cache_len, n_new, held_in, held_out, block_table, fre
 
 
 def _blocks(layer, q, q_out, k, v, slot_map):
+    _here(layer)
     L, dt = layer, _rows(layer)
     qs, ks = (L.batch, L.block, L.n_q_heads, L.head_dim), (L.batch, L.block, L.n_kv_heads, L.head_dim)
     _paged(slot_map, "slot_map", torch.int64, (L.batch, L.block))
@@ -189,11 +196,13 @@ def rope_paged_kv_write(layer, slot_map, q, k, v, rope_theta, q_out, workspace, 
 
 
 def paged_commit_len(layer, n_commit, workspace, stream):
+    _here(layer)
     _call("orthrus_paged_commit_len", ctypes.byref(layer), _paged(n_commit, "n_commit", torch.int32, (layer.batch,)),
           *_space(workspace), _stream(stream))
 
 
 def _paged_attend(name, layer, q, out, workspace, stream):
+    _here(layer)
     shape = (layer.batch, layer.block, layer.n_q_heads, layer.head_dim)
     qp, op = _paged(q, "q", _rows(layer), shape), _paged(out, "out", _rows(layer), shape)
     _call(name, ctypes.byref(layer), qp, op, *_space(workspace), _stream(stream))

@@ -63,6 +63,7 @@ class Layer(ctypes.Structure):
 
 class PagedLayer(ctypes.Structure):
     """Mirror of orthrus_paged_layer_t."""
+    device = None          # of the tensors it was made of (make_paged_layer); the calls refuse it on another one
     _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int64),
@@ -358,6 +359,7 @@ def make_paged_layer(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: 
                        v_pages.data_ptr(), block_table.data_ptr(), cache_len.data_ptr(),
                        None if n_new is None else n_new.data_ptr(), max_len_hint, softmax_scale, flags)
     layer.tensors = (k_pages, v_pages, block_table, cache_len, n_new)      # alive as long as the descriptor
+    layer.device = k_pages.device.index
     return layer
 
 

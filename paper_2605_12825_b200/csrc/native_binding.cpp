@@ -351,6 +351,17 @@ orthrus_paged_layer_t paged_layer_of(PyObject *o)
     }
     const orthrus_paged_layer_t L = *static_cast<const orthrus_paged_layer_t *>(view.buf);
     PyBuffer_Release(&view);
+    // where its tensors are; None if it was not made of tensors
+    PyObject *device = PyObject_GetAttrString(o, "device");
+    if (!device) throw Failed();
+    const long at = device == Py_None ? -1 : PyLong_AsLong(device);
+    const bool known = device != Py_None;
+    Py_DECREF(device);
+    if (at == -1 && PyErr_Occurred()) throw Failed();
+    if (known && at != c10::cuda::current_device()) {
+        PyErr_Format(PyExc_ValueError, "layer: on cuda:%ld, but the current device is cuda:%d", at, (int)c10::cuda::current_device());
+        throw Failed();
+    }
     return L;
 }
 at::ScalarType type_of(const orthrus_paged_layer_t &L) { return L.dtype == ORTHRUS_FP32 ? at::kFloat : at::kBFloat16; }
