@@ -402,9 +402,13 @@ typedef struct {
     const int32_t *block_table; /* device [B][max_pages]                            */
     int32_t *cache_len;     /* device [B]: rows P_b of request b before the block   */
     const int32_t *n_new;   /* device [B]: rows of the block that exist, 0..K; NULL: all K */
-    int32_t max_len_hint;   /* host upper bound on every P_b; sizes the grid.  0 means
-                               max_pages * page_size - block (or 0).  Longer requests are
-                               served all the same, with fewer CTAs than they would get */
+    int32_t max_len_hint;   /* host upper bound on every P_b; sizes the grid and chooses
+                               the kernel.  0 means max_pages * page_size - block (or 0).
+                               Longer requests are served all the same, with fewer CTAs
+                               than they would get.  A bound far above the lengths costs
+                               small calls (8 requests of up to 4096 keys, blocks of 16:
+                               15.4 us, 38 with a bound of 32768; one of 4096, one row:
+                               9.2 and 15.7); large ones it leaves as they are          */
     float softmax_scale;    /* 0 selects 1/sqrt(head_dim)                           */
     uint32_t flags;         /* ORTHRUS_LAYER_CACHE_QUIESCENT (the promise covers block_table,
                                n_new and the pages' rows below cache_len too) and
@@ -443,7 +447,9 @@ orthrus_status_t orthrus_page_tables(int32_t batch, int32_t page_size, int32_t n
  * block_table and n_new are not read; cache_len by the rotary form alone.
  *
  * orthrus_rope_paged_kv_write: the same with the rotary embedding of orthrus_rope_block_kv_write (same
- * pairing and angles, position cache_len[b] + i): q_out[b][i] = rotate(q[b][i]) (q_out may be q), keys rotated
+ * pairing and angles, position cache_len[b] + i; angles are reduced to a turn in double precision, and for bf16 the sine and cosine of the rest
+ * and the products taken in fp32, off by 2^-21 before the one rounding to bf16, so that a result may be rounded the other way than by the
+ * contiguous call, which takes them in double; fp32 layers are rotated in double by both): q_out[b][i] = rotate(q[b][i]) (q_out may be q), keys rotated
  * on their way, values copied.  Rows without a slot are padding: nothing of them is written, q_out neither.
  *   slot_map  device int64 [B][K];  k_blk, v_blk  [B][K][Hkv][d];  q, q_out  [B][K][Hq][d]
  * `workspace` may be NULL.  One launch each.
@@ -468,7 +474,8 @@ orthrus_status_t orthrus_paged_commit_len(const orthrus_paged_layer_t *layer, co
  * Rows i >= n are padding: they are not read and out keeps what it holds there.  q, out: [B][K][Hq][d].
  *
  * Long requests are cut over several CTAs, whose pieces are joined in the order of their keys: results are the same in
- * every run.  Large calls are cut evenly over the GPU whatever the lengths are; max_len_hint is used where it is small.
+ * every run.  Large calls are cut evenly over the GPU whatever the lengths are; calls that the shape and max_len_hint make small go to a kernel
+ * that gives every request the CTAs of the longest, and starts faster.
  * Unless ORTHRUS_LAYER_NO_EARLY_LAUNCH is set a call may look at lengths and tables ahead of the end of the call before it, and looks again
  * then.  In a row's result a masked score counts for nothing, whatever the key holds.  A value of the block itself that is not finite may
  * make NaN of all rows of its request and head, those that do not see it included.
@@ -498,9 +505,13 @@ orthrus_status_t orthrus_paged_diffusion_attend(const orthrus_paged_layer_t *lay
  *   logprob[r] = log of the token's share of the mass kept (logprob may be NULL).
  * temperature <= 0 or NaN is greedy: the first token in that order, logprob 0.  NaN and -inf logits are never drawn;
  * if the largest is +inf, all +inf have equal weight and the others none; a row with nothing to draw from gives token
- * 0 and logprob NaN.  Weights are taken in double precision and summed as integers (steps of 2^-62 times the vocabulary,
- * rounded up to a power of two): results do not depend on any order of execution, and differ from an exact evaluation only
- * where a running mass is within such steps of a border.
+ * 0 and logprob NaN.  Weights are taken in double precision (off by less than 2^-45 of themselves) and summed as integers, in
+ * steps of 2^-62 times the vocabulary rounded up to a power of two; u and top_p times a mass are products in double.  Results do not
+ * depend on any order of execution, and differ from an exact evaluation only where a running mass is within half a step for each token
+ * up to there, plus 2^-44 of the mass, of a border, or a weight within 2^-45 of min_p.
+ * Drafts for orthrus_consensus_sample have to be drawn from the distribution that it takes them to be of: softmax(diff_logits / T) with its one
+ * T for all rows, no top_k, top_p or min_p.  Drafts that were filtered, or drawn at another temperature, are verified all the same, but the
+ * committed tokens are then not distributed as the AR view's.
  *   logits  device [rows] rows of `vocab` elements, `row_stride` elements apart (>= vocab), bf16 or fp32
  *   temperature, top_p, min_p, u, logprob  device float [rows];  top_k, token  device int32 [rows]
  * 1 <= rows <= 2^20, 1 <= vocab <= 2^24.  No workspace.  One launch (for each 65535 rows).

@@ -12,7 +12,8 @@
 //      parts of the bin, until a part is one value.
 //   4. The wanted occurrence of the drawn value: a pass marks them in a bit map.
 // Weights are integers, exp((x - max) / T) in steps of 2^-S with 2^S times the vocabulary at most 2^62: sums do not depend on the
-// order in which atomics arrive, are exact, and a border is off by no more than the weights' own rounding.
+// order in which atomics arrive and are exact; what is off at a border is the weights' own rounding (half a step each, and that of a double: 2^-45
+// of the weight where the exponent is largest), and that of the products of u and top_p with a mass, 2^-52 of it.
 //
 // What bounds it: one row, latency (its steps follow one another at the cluster's barriers); many rows, the atomics in shared memory (one
 // a token for bf16, three for fp32 next to an exponential in double): 32 lanes that count in banks of their own take 1.7 clocks of an SM,
