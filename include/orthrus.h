@@ -448,7 +448,7 @@ orthrus_status_t orthrus_page_tables(int32_t batch, int32_t page_size, int32_t n
  *
  * orthrus_rope_paged_kv_write: the same with the rotary embedding of orthrus_rope_block_kv_write (same
  * pairing and angles, position cache_len[b] + i; angles are reduced to a turn in double precision, and for bf16 the sine and cosine of the rest
- * and the products taken in fp32, off by 2^-21 before the one rounding to bf16, so that a result may be rounded the other way than by the
+ * and the products taken in fp32, off by 2^-21 of a pair's length before the one rounding to bf16, so that a result may be rounded the other way than by the
  * contiguous call, which takes them in double; fp32 layers are rotated in double by both): q_out[b][i] = rotate(q[b][i]) (q_out may be q), keys rotated
  * on their way, values copied.  Rows without a slot are padding: nothing of them is written, q_out neither.
  *   slot_map  device int64 [B][K];  k_blk, v_blk  [B][K][Hkv][d];  q, q_out  [B][K][Hq][d]

@@ -10,7 +10,10 @@
 // are one cluster, with a barrier.
 //
 // What bounds it: latency (lengths, scan, list, slots: dependent steps, and a launch); for prompts the 8 bytes a slot.  256 requests that grow by 16
-// rows 8.1 us, 64 prompts of up to 8191 rows in pages of 64 6.5 us (4.2 MB of slots); in one cluster, as in place, 8.8 and 14.4.
+// rows 8.2 us, 64 prompts of up to 8191 rows in pages of 64 6.5 us (4.2 MB of slots); in one cluster, as in place, 8.8 and 14.4.  The former
+// has a hundredth of the slots and takes longer, because CTAs are as many as its slots ask for, two, and nine of its requests end: 4.7 us where no
+// page moves, 5.5 where each request takes one (a search for its place in the list, by every slot on it), 8.0 where those are pages that are given back in
+// the same call (a second search), 2250 in all; that on 32 CTAs 6.4.
 #include "paged.cuh"
 #include "tc_ptx.cuh"
 

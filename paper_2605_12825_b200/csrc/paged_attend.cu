@@ -23,6 +23,9 @@
 //   warp 5     MMAs: the scores of the next tile are issued ahead of the product of this one
 // A row's reference follows its maximum only when that has grown by more than 2^8 since: the output in tensor memory is rescaled rarely,
 // numerator and denominator use the same reference, and probabilities stay below 2^8.
+// Probabilities are rounded to bf16, the type of the values: the MMA takes operands of one type, and its rate with two products for each (a rounded
+// part and the rest) would be half.  The sum is of the unrounded ones.  Outputs are then off by 2.3e-3 of their size in the mean, where their own
+// rounding alone makes 1.7e-3 (2000 to 32768 keys).
 // Every wait is bounded: on expiry the CTA raises ORTHRUS_DEV_WAIT_TIMEOUT, waits for its copies and MMAs in flight and ends.
 #include <cuda.h>
 #include <type_traits>
@@ -516,6 +519,11 @@ int max_len_of(const orthrus_paged_layer_t &L)
 // 20.9, of 1000 to 8000 32.1 and 39.4 (all of 8000 48 and 43); 32 of 125 to 1000 25.2 and 20.9, of 250 to 2000 34.1 and 39.1; blocks of 16, 8 of 500
 // to 4000 34.8 and 24.9, 4 of 2000 to 16000 56 and 44, 8 of those 68 and 83; one KV head, 16000 and 60000 keys 20.4 and 19.5, 42 and 67.
 // Hence: up to 200 MB of keys and values at the bound (270 MB where rows are many), one request any number, and up to 12 tiles a CTA.
+// The host knows the bound and not the lengths, and the line is drawn for unequal ones, where the keys kernel loses most (30 of 32 requests of 1024 to 8192
+// keys 88 here and 157 there).  For equal ones it comes too early: 4 requests of 32768 keys, 64 query heads, 89.9 here and 78.4 there, call after call for
+// a second at 1785 MHz and 948 W, 1965 MHz and 689 W; 8 of 16000 with 64 rows 99 and 88.
+// A bound far above the lengths has its price too: 8 requests of 512 to 4096, blocks of 16, 4 KV heads, 15.4 us, 38 with a bound of 32768; one of
+// 4096 9.2 and 15.7.
 // ORTHRUS_TC_SMALL_ROWS=0 keeps all calls on this file's kernel, =1 puts there whatever fits (measurement knobs).
 int keys_plan(const orthrus_paged_layer_t &L)
 {
