@@ -481,6 +481,9 @@ orthrus_status_t orthrus_paged_commit_len(const orthrus_paged_layer_t *layer, co
  * make NaN of all rows of its request and head, those that do not see it included.
  * A cache_len or n_new out of range, or beyond what the table holds, is clamped (ORTHRUS_DEV_BAD_CACHE_LEN); a table entry outside the pool among those that
  * a request needs raises ORTHRUS_DEV_BAD_PAGE, is not followed, and leaves the request's outputs undefined.
+ * Sums over the keys are fp32.  Tensor cores cut them where others round, which takes about 6e-9 off an output for each key that one CTA sums up:
+ * far below bf16's rounding for requests of up to a million keys (0.01 to 0.03 % there), but 0.4 to 0.8 % at 20 million and 3 to 5 % at
+ * 140 million.  The plain arithmetic (orthrus_set_path("simt")) loses nothing of the kind.
  * Workspace: orthrus_paged_attend_workspace_bytes(layer), initialised by orthrus_workspace_init once.  It depends on the
  * shape, on max_len_hint and on the device, not on the lengths.  Calls of other shapes and kinds on the same stream may share it.
  * 1 <= batch <= 16384.
